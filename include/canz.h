@@ -41,7 +41,7 @@ enum {
 
 enum { CANZ_COST_NUMEL = 0, CANZ_COST_NS_FLOPS = 1, CANZ_COST_SHAMPOO_FLOPS = 2, CANZ_COST_SOAP_FLOPS = 3 };
 #define CANZ_SOAP_COST_MAX_PRECOND_DIM 10000 /* the limit CANZ_COST_SOAP_FLOPS assumes for canz_soap_hparams.max_precond_dim */
-enum { CANZ_DT_F32 = 0, CANZ_DT_BF16 = 1 };
+enum { CANZ_DT_F32 = 0, CANZ_DT_BF16 = 1, CANZ_DT_MX = 2 /* a microscaled image: a_dtype of canz_mx_product only */ };
 enum { CANZ_SCALE_NONE = 0, CANZ_SCALE_ASPECT = 1, CANZ_SCALE_RMS = 2 };
 enum { CANZ_PREC_BF16 = 0, CANZ_PREC_F32 = 1 };
 enum { CANZ_OUT_PARAM = 0, CANZ_OUT_DELTA = 1 };
@@ -450,6 +450,119 @@ int canz_muon_step_static(const canz_group* g, int32_t n_groups, const canz_muon
                           void* hip_stream);
 
 /*
+ * Microscaled 4-bit images (MXFP4) of matrices, and their products.
+ *
+ * Beside the step: a rank can hand out the parameters it has updated as images of 17/32 bytes an element, one for each of the
+ * products a linear layer takes them into, and the gradients that enter a step come out of products of such images:
+ *   y = x W^T        x by_row (tokens x in)    W by_row (out x in)
+ *   dx = dy W        dy by_row (tokens x out)  W by_col (an in x out image)
+ *   dW = dy^T x      dy by_col (out x tokens)  x by_col (in x tokens)
+ *
+ * An image of R rows and K columns is the rounded matrix as operand of a product that contracts over the columns.  Every 32
+ * consecutive elements of a row (the last ones of a row may be fewer) are a block with a common X, a power of two in an E8M0
+ * byte (2^(byte - 127)), and each of them is held in 4 bits (E2M1) as one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 with a sign, times X.  With
+ * amax the largest magnitude of the block:
+ *   CANZ_MX_SCALE_FLOOR  X = 2^(floor(log2 amax) - 2), the rule of the OCP microscaling formats; what is above 6 X becomes 6 X
+ *   CANZ_MX_SCALE_CEIL   X = the smallest power of two with amax <= 6 X; nothing saturates
+ * and 2^-127 <= X <= 2^125 in either case (small elements are held at the spacing 2^-128; every value is finite in fp32 and in
+ * bf16, and CANZ_MX_SCALE_CEIL saturates above 6 2^125 = 2.55e38).  Without noise an element v becomes
+ * the nearest of these values, ties to the even code.  With a noise byte u and the distance s of the values around a = |v| / X
+ * (0.5 below 2, 1 below 4, 2 above) its magnitude becomes X min(6, s floor((rint(256 a / s) + u) / 256)): u uniform in 0 .. 255
+ * gives v itself in the mean, to within s X / 512 (and but for the saturation of CANZ_MX_SCALE_FLOOR).  A block that holds an
+ * infinity or a NaN is NaN as a whole (X is), and so is every element of a product that it enters.
+ *
+ * The layout of an image is the matrix cores' and fixed: rows padded to 64 and columns to 128, codes first (units of 16 rows x 128
+ * columns), then scale bytes; images are made by canz_mx_quantize and read by the calls below, and may be copied and sent as
+ * canz_mx_image_bytes() bytes.  Images and the workspace must be 256-byte aligned, matrices 16-byte aligned (at their first
+ * element; rows may lie any number of elements apart, at least their length); noise may lie anywhere.  Extents are at most
+ * 4194240 each and padded matrices at most 2^37 elements; an extent may be 0, and then nothing is read or written (k = 0 in a product:
+ * C <- beta C) and the pointers of that matrix may be NULL.  Tables are host arrays of device pointers, read during the call.
+ * The calls issue kernel launches only (no allocation, copy, memset or synchronisation), on the device hip_stream
+ * belongs to (NULL: the current one), and may be recorded into a HIP graph.  Results do not depend on what else is in the call.
+ */
+enum { CANZ_MX_SCALE_FLOOR = 0, CANZ_MX_SCALE_CEIL = 1 };
+
+/* Bytes of an image of `rows` rows and `cols` columns (a multiple of 256; 0 if an extent is 0). */
+int canz_mx_image_bytes(int64_t rows, int64_t cols, size_t* bytes_out);
+
+/* Matrices of one shape and type with their images. */
+typedef struct {
+  int64_t rows, cols;
+  int64_t ld;                /* elements from a row of mat to the next, >= cols                          */
+  int32_t n_mats;
+  int32_t dtype;             /* CANZ_DT_F32 or CANZ_DT_BF16                                              */
+  void* const* mat;          /* [n_mats]                                                                 */
+  void* const* by_row;       /* [n_mats] images of rows x cols, or NULL                                  */
+  void* const* by_col;       /* [n_mats] images of the transposes, cols x rows, or NULL                  */
+  const void* const* noise;  /* [n_mats] rows x cols bytes, dense, or NULL; one byte serves both images  */
+} canz_mx_group;
+
+/*
+ * canz_mx_quantize - enqueue the images of the given matrices on hip_stream; both images of a matrix from one reading of it.
+ * Errors: CANZ_EINVAL (null or misaligned pointers, n_mats < 0, negative extents, ld < cols, neither image asked for),
+ * CANZ_ESHAPE (an extent or a matrix above the limits), CANZ_EUNSUPPORTED (dtype, scale_mode), CANZ_EHIP (earlier groups may be
+ * enqueued already); all but the last before anything is enqueued.
+ */
+int canz_mx_quantize(const canz_mx_group* g, int32_t n_groups, int32_t scale_mode, void* hip_stream);
+
+/*
+ * canz_mx_dequantize - enqueue the way back: mat receives the values that its image stands for, from by_row or from by_col (exactly
+ * one of them given; mat is rows x cols in either case).  Exact in fp32 and in bf16; elements of mat between cols and ld stay as they
+ * are.  noise is not looked at.  Errors as canz_mx_quantize.
+ */
+int canz_mx_dequantize(const canz_mx_group* g, int32_t n_groups, void* hip_stream);
+
+/*
+ * Products of one shape: C = alpha A B^T + beta C with A (m x k) and B (n x k).  B is an image.  A is an image (CANZ_DT_MX) or a
+ * row-major matrix that the call rounds as canz_mx_quantize does, to the nearest values with a_scale_mode; the result is the same.
+ * Products of two elements are exact, sums over k are in fp32 (their order depends on m, n and k alone), and an element is rounded once to the type of
+ * C.  C is not read where beta is 0.  C must not overlap another buffer of the call.
+ */
+typedef struct {
+  int64_t m, n, k;
+  int64_t lda;               /* elements from a row of A to the next, >= k; not looked at for images */
+  int64_t ldc;               /* elements from a row of C to the next, >= n                           */
+  int32_t n_prods;
+  int32_t a_dtype;           /* CANZ_DT_F32, CANZ_DT_BF16 or CANZ_DT_MX                              */
+  int32_t out_dtype;         /* CANZ_DT_F32 or CANZ_DT_BF16                                          */
+  int32_t a_scale_mode;      /* CANZ_MX_SCALE_*, for matrices                                        */
+  float alpha, beta;
+  const void* const* a;      /* [n_prods]                                                            */
+  const void* const* b;      /* [n_prods] images                                                     */
+  void* const* c;            /* [n_prods]                                                            */
+} canz_mx_product_group;
+
+/* Device scratch canz_mx_product needs for these groups (at least 256).  Pointer tables may be NULL for this call. */
+int canz_mx_product_workspace_bytes(const canz_mx_product_group* g, int32_t n_groups, size_t* bytes_out);
+
+/*
+ * canz_mx_product - enqueue the given products on hip_stream; groups may differ in every extent (experts with the rows a router gave
+ * them), and all products of a call may run at once.
+ *   workspace       device, 256-byte aligned, caller-owned scratch that need not be initialised; not to be shared by calls that may
+ *                   run at the same time (two streams, two graphs)
+ * Errors: CANZ_EINVAL, CANZ_ESHAPE, CANZ_EUNSUPPORTED, CANZ_EHIP as canz_mx_quantize; CANZ_EWORKSPACE.
+ */
+int canz_mx_product(const canz_mx_product_group* g, int32_t n_groups, void* workspace, size_t workspace_bytes,
+                    void* hip_stream);
+
+/* The images of one canz_group's parameters (both NULL: none are taken of that group). */
+typedef struct {
+  void* const* by_row;       /* [n_mats] rows x cols, or NULL */
+  void* const* by_col;       /* [n_mats] cols x rows, or NULL */
+} canz_mx_images;
+
+/*
+ * canz_muon_step_images - canz_muon_step that leaves images of the updated parameters (what the ranks then exchange, Sec. 3.3
+ * stage (3), in a quarter of the bytes of bf16): the step, with the same results, then canz_mx_quantize on its out buffers, in stream order.
+ *   images          host array [n_groups]
+ * Errors: those of the two calls, all but CANZ_EHIP before anything is enqueued; CANZ_EUNSUPPORTED if hp->out_mode is not
+ * CANZ_OUT_PARAM.
+ */
+int canz_muon_step_images(const canz_group* g, int32_t n_groups, const canz_muon_hparams* hp,
+                          const canz_mx_images* images, int32_t scale_mode,
+                          void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
  * Per-kernel timing of canz_muon_step / canz_shampoo_step / canz_soap_step, for benchmarks (the measurement protocol of
  * App. C.1 reports the optimizer time; this splits it by kernel).  While enabled, every
  * kernel launch of a step is bracketed by a pair of HIP events on the step's own stream.
@@ -462,6 +575,7 @@ int canz_muon_step_static(const canz_group* g, int32_t n_groups, const canz_muon
  *                         launch counts per kernel kind into ms_out / launches_out
  *                         (host arrays of CANZ_KERNEL_KINDS entries) and starts a new period.
  *   canz_profile_disable  stops recording.
+ * The launches of canz_mx_* are not recorded.
  */
 enum {
   CANZ_KERNEL_MOMENTUM = 0, /* momentum + gather + cast + norm partial sums */

@@ -24,6 +24,9 @@ soap        The SOAP operator of the same experiment: Adam in the eigenbasis of 
 muon        The Muon operator named in Sec. 4.1 / App. B.3: momentum,
             Frobenius normalisation, k Newton-Schulz steps, scaled update;
             TP column-fragment gather/scatter of Sec. 4.1 stages (1) and (3).
+mx          Microscaled 4-bit images (blocks of 32 with a power-of-two scale, E2M1 elements):
+            rounding by comparison with the eight magnitudes, the storage layout, products
+            in fp64.
 
 Parity pins (tests/test_oracle_*.py): every function here is pinned to
 something other than itself - SVD closed forms and the polar factor for the

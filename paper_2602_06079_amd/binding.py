@@ -20,14 +20,17 @@ LIB_PATH = os.path.join(_HERE, "libcanz.so")
 
 OK, EINVAL, ESHAPE, EWORKSPACE, EHIP, EUNSUPPORTED = 0, -1, -2, -3, -4, -5
 COST_NUMEL, COST_NS_FLOPS, COST_SHAMPOO_FLOPS, COST_SOAP_FLOPS = 0, 1, 2, 3
-DT_F32, DT_BF16 = 0, 1
+DT_F32, DT_BF16, DT_MX = 0, 1, 2
 SCALE_NONE, SCALE_ASPECT, SCALE_RMS = 0, 1, 2
 PREC_BF16, PREC_F32 = 0, 1
 OUT_PARAM, OUT_DELTA = 0, 1
+MX_SCALE_FLOOR, MX_SCALE_CEIL = 0, 1
 
 EXPORTS = ("canz_last_error", "canz_version", "canz_partition_alpha", "canz_partition_naive", "canz_microgroup_plan", "canz_tp_schedule",
            "canz_muon_workspace_bytes", "canz_muon_step", "canz_muon_step_static",
            "canz_shampoo_workspace_bytes", "canz_shampoo_step", "canz_soap_workspace_bytes", "canz_soap_step",
+           "canz_mx_image_bytes", "canz_mx_quantize", "canz_mx_dequantize", "canz_mx_product_workspace_bytes", "canz_mx_product",
+           "canz_muon_step_images",
            "canz_profile_enable", "canz_profile_collect", "canz_profile_disable")
 KERNEL_KINDS = ("momentum", "norm", "gram", "poly", "update", "final", "apply",
                 "sh_load", "sh_stat", "sh_init", "sh_root", "sh_apply",
@@ -81,6 +84,23 @@ class _SoapHparams(C.Structure):
                 ("bf16_rotations", C.c_int32)]
 
 
+class _MxGroup(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("ld", C.c_int64), ("n_mats", C.c_int32), ("dtype", C.c_int32),
+                ("mat", C.POINTER(C.c_void_p)), ("by_row", C.POINTER(C.c_void_p)), ("by_col", C.POINTER(C.c_void_p)),
+                ("noise", C.POINTER(C.c_void_p))]
+
+
+class _MxProduct(C.Structure):
+    _fields_ = [("m", C.c_int64), ("n", C.c_int64), ("k", C.c_int64), ("lda", C.c_int64), ("ldc", C.c_int64),
+                ("n_prods", C.c_int32), ("a_dtype", C.c_int32), ("out_dtype", C.c_int32), ("a_scale_mode", C.c_int32),
+                ("alpha", C.c_float), ("beta", C.c_float),
+                ("a", C.POINTER(C.c_void_p)), ("b", C.POINTER(C.c_void_p)), ("c", C.POINTER(C.c_void_p))]
+
+
+class _MxImages(C.Structure):
+    _fields_ = [("by_row", C.POINTER(C.c_void_p)), ("by_col", C.POINTER(C.c_void_p))]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise RuntimeError("libcanz.so is missing at %s - build it with "
@@ -126,6 +146,19 @@ def _load():
     lib.canz_soap_step.argtypes = [C.POINTER(_SoapGroup), C.c_int32, C.POINTER(_SoapHparams), C.c_void_p, C.c_size_t,
                                    C.c_void_p]
     lib.canz_soap_step.restype = C.c_int
+    lib.canz_mx_image_bytes.argtypes = [C.c_int64, C.c_int64, C.POINTER(C.c_size_t)]
+    lib.canz_mx_image_bytes.restype = C.c_int
+    lib.canz_mx_quantize.argtypes = [C.POINTER(_MxGroup), C.c_int32, C.c_int32, C.c_void_p]
+    lib.canz_mx_quantize.restype = C.c_int
+    lib.canz_mx_dequantize.argtypes = [C.POINTER(_MxGroup), C.c_int32, C.c_void_p]
+    lib.canz_mx_dequantize.restype = C.c_int
+    lib.canz_mx_product_workspace_bytes.argtypes = [C.POINTER(_MxProduct), C.c_int32, C.POINTER(C.c_size_t)]
+    lib.canz_mx_product_workspace_bytes.restype = C.c_int
+    lib.canz_mx_product.argtypes = [C.POINTER(_MxProduct), C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.canz_mx_product.restype = C.c_int
+    lib.canz_muon_step_images.argtypes = [C.POINTER(_Group), C.c_int32, C.POINTER(_Hparams), C.POINTER(_MxImages), C.c_int32,
+                                          C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.canz_muon_step_images.restype = C.c_int
     lib.canz_profile_enable.argtypes = [C.c_int32]
     lib.canz_profile_enable.restype = C.c_int
     lib.canz_profile_collect.argtypes = [C.POINTER(C.c_double), i64p]
@@ -432,6 +465,126 @@ def canz_muon_step_static(groups: Sequence[Group], hp: Hparams, stream=0) -> Non
     arr, _keep = _marshal(groups)
     h = hp._c()
     _check(_lib.canz_muon_step_static(arr, len(groups), C.byref(h), C.c_void_p(int(stream))))
+
+
+def canz_mx_image_bytes(rows: int, cols: int) -> int:
+    """Bytes of a microscaled image of ``rows`` rows and ``cols`` columns."""
+    out = C.c_size_t(0)
+    _check(_lib.canz_mx_image_bytes(int(rows), int(cols), C.byref(out)))
+    return int(out.value)
+
+
+@dataclass
+class MxGroup:
+    """Matrices of one shape and their microscaled images: device buffers given as addresses or objects with data_ptr()."""
+    rows: int
+    cols: int
+    mat: Sequence = field(default_factory=list)      # n_mats
+    by_row: Sequence = field(default_factory=list)   # n_mats images of rows x cols, or empty
+    by_col: Sequence = field(default_factory=list)   # n_mats images of cols x rows (the transposes), or empty
+    noise: Sequence = field(default_factory=list)    # n_mats, rows x cols bytes, or empty: round to nearest
+    dtype: int = DT_F32
+    ld: int = -1                                     # -1: cols
+    n_mats: int = -1                                 # -1: len(mat)
+
+
+@dataclass
+class MxProduct:
+    """Products of one shape, C = alpha A B^T + beta C: device buffers given as addresses or objects with data_ptr()."""
+    m: int
+    n: int
+    k: int
+    a: Sequence = field(default_factory=list)        # n_prods, m x k: images, or matrices (a_dtype)
+    b: Sequence = field(default_factory=list)        # n_prods images of n x k
+    c: Sequence = field(default_factory=list)        # n_prods, m x n
+    a_dtype: int = DT_MX
+    out_dtype: int = DT_BF16
+    alpha: float = 1.0
+    beta: float = 0.0
+    a_scale_mode: int = MX_SCALE_FLOOR
+    lda: int = -1                                    # -1: k
+    ldc: int = -1                                    # -1: n
+    n_prods: int = -1                                # -1: len(c)
+
+
+_NO_TABLE = C.POINTER(C.c_void_p)()
+
+
+def _table(seq, keep, n):
+    """The host table of n device addresses; empty: a null table."""
+    if not len(seq):
+        return _NO_TABLE
+    if len(seq) != n:
+        raise ValueError("a table of %d buffers where the group has %d" % (len(seq), n))
+    t = (C.c_void_p * len(seq))(*[_addr(x) for x in seq])
+    keep.append(t)
+    return C.cast(t, C.POINTER(C.c_void_p))
+
+
+def _marshal_mx(groups: Sequence[MxGroup]):
+    arr = (_MxGroup * max(len(groups), 1))()
+    keep = []
+    for i, g in enumerate(groups):
+        n = len(g.mat) if g.n_mats == -1 else g.n_mats
+        arr[i] = _MxGroup(g.rows, g.cols, g.cols if g.ld == -1 else g.ld, n, g.dtype,
+                          _table(g.mat, keep, n), _table(g.by_row, keep, n), _table(g.by_col, keep, n), _table(g.noise, keep, n))
+    return arr, keep
+
+
+def _marshal_mx_product(groups: Sequence[MxProduct]):
+    arr = (_MxProduct * max(len(groups), 1))()
+    keep = []
+    for i, g in enumerate(groups):
+        n = len(g.c) if g.n_prods == -1 else g.n_prods
+        arr[i] = _MxProduct(g.m, g.n, g.k, g.k if g.lda == -1 else g.lda, g.n if g.ldc == -1 else g.ldc, n, g.a_dtype, g.out_dtype,
+                            g.a_scale_mode, g.alpha, g.beta, _table(g.a, keep, n), _table(g.b, keep, n), _table(g.c, keep, n))
+    return arr, keep
+
+
+def canz_mx_quantize(groups: Sequence[MxGroup], scale_mode: int = MX_SCALE_FLOOR, stream=0) -> None:
+    """Enqueue the microscaled images of the given matrices on ``stream``."""
+    arr, _keep = _marshal_mx(groups)
+    _check(_lib.canz_mx_quantize(arr, len(groups), int(scale_mode), C.c_void_p(int(stream))))
+
+
+def canz_mx_dequantize(groups: Sequence[MxGroup], stream=0) -> None:
+    """Enqueue the values that the given images (by_row or by_col) stand for, into mat."""
+    arr, _keep = _marshal_mx(groups)
+    _check(_lib.canz_mx_dequantize(arr, len(groups), C.c_void_p(int(stream))))
+
+
+def canz_mx_product_workspace_bytes(groups: Sequence[MxProduct]) -> int:
+    arr, _keep = _marshal_mx_product(groups)
+    out = C.c_size_t(0)
+    _check(_lib.canz_mx_product_workspace_bytes(arr, len(groups), C.byref(out)))
+    return int(out.value)
+
+
+def canz_mx_product(groups: Sequence[MxProduct], workspace, workspace_bytes: int, stream=0) -> None:
+    """Enqueue the given products of microscaled images on ``stream``."""
+    arr, _keep = _marshal_mx_product(groups)
+    _check(_lib.canz_mx_product(arr, len(groups), C.c_void_p(_addr(workspace)), int(workspace_bytes), C.c_void_p(int(stream))))
+
+
+@dataclass
+class MxImages:
+    """Images of the parameters of one Group for canz_muon_step_images."""
+    by_row: Sequence = field(default_factory=list)   # one per matrix of the group, or empty
+    by_col: Sequence = field(default_factory=list)
+
+
+def canz_muon_step_images(groups: Sequence[Group], hp: Hparams, images: Sequence[MxImages], scale_mode: int, workspace,
+                          workspace_bytes: int, stream=0) -> None:
+    """canz_muon_step that leaves microscaled images of the updated parameters (images[i] belongs to groups[i])."""
+    if len(images) != len(groups):
+        raise ValueError("images: one entry per group")
+    arr, _keep = _marshal(groups)
+    keep = []
+    im = (_MxImages * max(len(images), 1))(*[_MxImages(_table(x.by_row, keep, arr[i].n_mats), _table(x.by_col, keep, arr[i].n_mats))
+                                             for i, x in enumerate(images)])
+    h = hp._c()
+    _check(_lib.canz_muon_step_images(arr, len(groups), C.byref(h), im, int(scale_mode), C.c_void_p(_addr(workspace)),
+                                      int(workspace_bytes), C.c_void_p(int(stream))))
 
 
 def canz_profile_enable(max_launches: int) -> None:

@@ -1,0 +1,68 @@
+// Launchers behind the canz_mx_* entry points (internal, not part of the ABI).
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "canz.h"
+#include "mx_layout.h"
+
+namespace canz {
+
+// Kernels are launched on the device the caller's stream belongs to, whatever the thread's current device is.
+class StreamDevice {
+ public:
+  explicit StreamDevice(hipStream_t st) {
+    hipDevice_t dev = 0;
+    if (st == nullptr) return;   // the null stream belongs to the current device
+    if ((err_ = hipStreamGetDevice(st, &dev)) != hipSuccess || (err_ = hipGetDevice(&before_)) != hipSuccess) return;
+    if (dev != before_) restore_ = (err_ = hipSetDevice(dev)) == hipSuccess;
+  }
+  ~StreamDevice() {
+    if (restore_) (void)hipSetDevice(before_);
+  }
+  StreamDevice(const StreamDevice&) = delete;
+  StreamDevice& operator=(const StreamDevice&) = delete;
+  hipError_t error() const { return err_; }
+
+ private:
+  int before_ = 0;
+  bool restore_ = false;
+  hipError_t err_ = hipSuccess;
+};
+
+// Matrices of one shape in one launch.
+constexpr int MX_MAX_MATS = 32;
+struct MxMats {
+  int64_t rows, cols, ld;
+  int n, dtype, scale_mode;
+  void* mat[MX_MAX_MATS];
+  uint8_t* by_row[MX_MAX_MATS];       // all null or none
+  uint8_t* by_col[MX_MAX_MATS];
+  const uint8_t* noise[MX_MAX_MATS];
+};
+hipError_t launch_mx_quantize(const MxMats& m, hipStream_t st);
+hipError_t launch_mx_dequantize(const MxMats& m, hipStream_t st);
+
+// C = alpha A B^T + beta C of images A (m x k) and B (n x k), several products in one launch.
+struct MxProblem {
+  const uint8_t *a, *b;
+  void* c;
+  int64_t m, n, k, ldc;
+  float alpha, beta;
+  int out_dtype;
+  int first_tile;   // set by the launcher
+};
+constexpr int MX_MAX_PROBLEMS = 32;
+struct MxProblems {
+  int n;
+  MxProblem pr[MX_MAX_PROBLEMS];
+};
+hipError_t launch_mx_product(MxProblems& p, hipStream_t st);
+
+// Validates one group of canz_mx_quantize (`back`: of canz_mx_dequantize).
+int check_mx_group(const canz_mx_group& g, int idx, bool back);
+// The images of a checked group, in launches of MX_MAX_MATS matrices.
+int quantize_group(const canz_mx_group& g, int scale_mode, hipStream_t st);
+
+}  // namespace canz

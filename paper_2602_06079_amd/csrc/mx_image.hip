@@ -1,0 +1,288 @@
+// Microscaled 4-bit images of matrices: canz_mx_quantize and canz_mx_dequantize.
+//
+// A block of 32 consecutive elements along the contracted index shares a scale X = 2^e; an element is one of 0, .5, 1, 1.5, 2, 3, 4,
+// 6 times X.  X follows from the largest magnitude's bits: with biased exponent E the floor rule takes E - 2, the ceil rule one more
+// where the mantissa is above 1.5, neither less than 0 (2^-127).  Division by X is exact, and the conversion instruction rounds to the
+// nearest value, ties to the even code, at most 6 (v_cvt_scalef32_pk_fp4_f32; it reads the exponent field of its scale alone, so that byte << 23 is
+// 2^(byte - 127) for every byte).  The ceil rule's X stops at 2^125, where the floor rule's ends by itself.
+#include "device_util.h"
+#include "mx.h"
+
+namespace canz {
+namespace {
+
+constexpr int TILE = 128;      // rows and columns of a block's tile: whole units of codes and of scales for either image
+constexpr int THREADS = 256;
+constexpr unsigned NONFINITE = 0x7F800000u;   // magnitudes with these bits or above are infinite or NaN
+constexpr unsigned SCALE_NAN = 255u;
+constexpr int MAX_SCALE = 252;                // 2^125: six times it is the largest value that fp32 holds
+
+typedef unsigned u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+// scale byte of a block whose largest magnitude has the bits `amax`
+__device__ __forceinline__ unsigned scale_byte(unsigned amax, bool ceil) {
+  if (amax >= NONFINITE) return SCALE_NAN;
+  const int e = static_cast<int>(amax >> 23) - 2 + (ceil && (amax & 0x7FFFFFu) > 0x400000u ? 1 : 0);
+  return static_cast<unsigned>(min(max(e, 0), MAX_SCALE));
+}
+__device__ __forceinline__ float scale_value(unsigned byte) { return __builtin_bit_cast(float, byte << 23); }
+
+// Code of one element with noise u in 0 .. 255: s floor((rint(256 a / s) + u) / 256) for a = |v| / X and the distance s of the values
+// around it.  Every step before the rint is exact, and it and the sum are integers below 2^11.
+__device__ __forceinline__ unsigned noisy_code(float v, unsigned byte, unsigned u) {
+  const float a = __builtin_amdgcn_ldexpf(__builtin_fabsf(v), 127 - static_cast<int>(byte));
+  const int shift = a < 2.f ? 9 : a < 4.f ? 8 : 7;
+  const unsigned n = (static_cast<unsigned>(__builtin_rintf(__builtin_amdgcn_ldexpf(a, shift))) + u) >> 8;
+  const unsigned code = min(n + (a < 2.f ? 0u : a < 4.f ? 2u : 4u), 7u);
+  return code | (__builtin_bit_cast(unsigned, v) >> 31 << 3);
+}
+// eight codes of one block, element 0 in the lowest bits
+template <bool NOISE>
+__device__ __forceinline__ unsigned eight_codes(const float (&v)[8], unsigned byte, unsigned long long noise) {
+  if (byte == SCALE_NAN) return 0;
+  unsigned r = 0;
+  if constexpr (NOISE) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r |= noisy_code(v[i], byte, static_cast<unsigned>(noise >> (8 * i)) & 255u) << (4 * i);
+  } else {
+    const float s = scale_value(byte);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[0], v[1], s, 0);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[2], v[3], s, 1);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[4], v[5], s, 2);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[6], v[7], s, 3);
+  }
+  return r;
+}
+__device__ __forceinline__ unsigned magnitude(float v) { return __builtin_bit_cast(unsigned, v) & 0x7FFFFFFFu; }
+
+// eight consecutive elements of a row, those behind its end as zeros
+template <typename E>
+__device__ __forceinline__ void load8(const E* p, int64_t left, float (&v)[8]) {
+  if (left >= 8) {
+    if constexpr (sizeof(E) == 4) {
+      const f32x4_any a = *reinterpret_cast<const f32x4_any*>(p), b = *reinterpret_cast<const f32x4_any*>(p + 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+    } else {
+      const bf16x8_any a = *reinterpret_cast<const bf16x8_any*>(p);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = static_cast<float>(a[i]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < left ? static_cast<float>(p[i]) : 0.f;
+  }
+}
+__device__ __forceinline__ unsigned long long load_noise8(const uint8_t* p, int64_t left) {
+  if (left >= 8) return __builtin_bit_cast(unsigned long long, *reinterpret_cast<const u32x2_any*>(p));
+  unsigned long long r = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r |= i < left ? static_cast<unsigned long long>(p[i]) << (8 * i) : 0ull;
+  return r;
+}
+template <typename E>
+__device__ __forceinline__ void store8(E* p, int64_t left, const float (&v)[8]) {
+  if (left >= 8) {
+    if constexpr (sizeof(E) == 4) {
+      f32x4_any a, b;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[i] = v[i], b[i] = v[4 + i];
+      *reinterpret_cast<f32x4_any*>(p) = a, *reinterpret_cast<f32x4_any*>(p + 4) = b;
+    } else {
+      bf16x8_any a;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) a[i] = static_cast<__bf16>(v[i]);
+      *reinterpret_cast<bf16x8_any*>(p) = a;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < left) p[i] = static_cast<E>(v[i]);
+  }
+}
+
+// One block rounds a tile of 128 x 128 elements: first along its rows (16 lanes a row, 8 elements each, 4 lanes a block), keeping
+// the elements in LDS, then along its columns (a thread a block).  Scale bytes are collected in LDS and leave as whole units.
+template <typename E, bool ROW, bool COL, bool NOISE>
+__global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {
+  __shared__ E tile[COL ? TILE * TILE : 1];
+  __shared__ uint8_t tile_noise[COL && NOISE ? TILE * TILE : 1];
+  __shared__ unsigned scales[2][2][MX_SCALE_BYTES / 4];
+  const int t = threadIdx.x, which = blockIdx.y;
+  const int64_t tiles_c = (m.cols + TILE - 1) / TILE;
+  const int64_t r0 = blockIdx.x / tiles_c * TILE, c0 = blockIdx.x % tiles_c * TILE;
+  const E* const src = static_cast<const E*>(m.mat[which]);
+  const uint8_t* const noise = NOISE ? m.noise[which] : nullptr;
+  const bool ceil = m.scale_mode == CANZ_MX_SCALE_CEIL;
+  const int64_t units_row = mx_k_units(m.cols), units_col = mx_k_units(m.rows);   // k units of the two images
+
+  const int col = (t & 15) * 8;
+#pragma unroll 4
+  for (int i = 0; i < TILE / 16; ++i) {
+    const int row = i * 16 + (t >> 4);
+    const int64_t left = r0 + row < m.rows ? m.cols - (c0 + col) : 0;
+    float v[8];
+    load8(src + (r0 + row) * m.ld + c0 + col, left, v);
+    unsigned long long u = 0;
+    if constexpr (NOISE) u = load_noise8(noise + (r0 + row) * m.cols + c0 + col, left);
+    if constexpr (COL) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) tile[row * TILE + col + e] = static_cast<E>(v[e]);
+      if constexpr (NOISE) *reinterpret_cast<unsigned long long*>(tile_noise + row * TILE + col) = u;
+    }
+    if constexpr (ROW) {
+      unsigned amax = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) amax = max(amax, magnitude(v[e]));
+      amax = max(amax, static_cast<unsigned>(__shfl_xor(static_cast<int>(amax), 1, 64)));
+      amax = max(amax, static_cast<unsigned>(__shfl_xor(static_cast<int>(amax), 2, 64)));
+      const unsigned byte = scale_byte(amax, ceil);
+      const unsigned codes = eight_codes<NOISE>(v, byte, u);
+      const int kb = (t & 15) >> 2;
+      const int64_t rt = (r0 + row) / MX_UNIT_ROWS;
+      if (rt < mx_row_tiles(m.rows))
+        *reinterpret_cast<unsigned*>(m.by_row[which] + (rt * units_row + c0 / MX_UNIT_K) * MX_UNIT_BYTES + (kb * 16 + row % 16) * 16 +
+                                     (t & 3) * 4) = codes;
+      if ((t & 3) == 0) reinterpret_cast<uint8_t*>(scales[0][row >> 6])[(kb * 16 + row % 16) * 4 + (row >> 4) % 4] = static_cast<uint8_t>(byte);
+    }
+  }
+  __syncthreads();
+  if constexpr (COL) {
+    const int c = t & (TILE - 1);
+    const int64_t rt = (c0 + c) / MX_UNIT_ROWS;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int rb = (t >> 7) + 2 * i;
+      unsigned amax = 0;
+#pragma unroll
+      for (int e = 0; e < MX_BLOCK; ++e) amax = max(amax, magnitude(static_cast<float>(tile[(rb * MX_BLOCK + e) * TILE + c])));
+      const unsigned byte = scale_byte(amax, ceil);
+      u32x4 codes;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float v[8];
+        unsigned long long u = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int at = (rb * MX_BLOCK + q * 8 + e) * TILE + c;
+          v[e] = static_cast<float>(tile[at]);
+          if constexpr (NOISE) u |= static_cast<unsigned long long>(tile_noise[at]) << (8 * e);
+        }
+        codes[q] = eight_codes<NOISE>(v, byte, u);
+      }
+      if (rt < mx_row_tiles(m.cols))
+        *reinterpret_cast<u32x4*>(m.by_col[which] + (rt * units_col + r0 / MX_UNIT_K) * MX_UNIT_BYTES + (rb * 16 + c % 16) * 16) = codes;
+      reinterpret_cast<uint8_t*>(scales[1][c >> 6])[(rb * 16 + c % 16) * 4 + (c >> 4) % 4] = static_cast<uint8_t>(byte);
+    }
+    __syncthreads();
+  }
+  const int half = (t >> 6) & 1, word = t & 63;
+  if (ROW && t < 128 && r0 + half * MX_PAD_ROWS < m.rows)
+    *reinterpret_cast<unsigned*>(m.by_row[which] + mx_code_bytes(m.rows, m.cols) +
+                                 ((r0 / MX_PAD_ROWS + half) * units_row + c0 / MX_UNIT_K) * MX_SCALE_BYTES + word * 4) = scales[0][half][word];
+  if (COL && t >= 128 && c0 + half * MX_PAD_ROWS < m.cols)
+    *reinterpret_cast<unsigned*>(m.by_col[which] + mx_code_bytes(m.cols, m.rows) +
+                                 ((c0 / MX_PAD_ROWS + half) * units_col + r0 / MX_UNIT_K) * MX_SCALE_BYTES + word * 4) = scales[1][half][word];
+}
+
+__device__ __forceinline__ void eight_values(unsigned codes, unsigned byte, float (&v)[8]) {
+  const float s = scale_value(byte == SCALE_NAN ? 127u : byte);
+  const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 1);
+  const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 3);
+  v[0] = a[0], v[1] = a[1], v[2] = b[0], v[3] = b[1], v[4] = c[0], v[5] = c[1], v[6] = d[0], v[7] = d[1];
+  if (byte == SCALE_NAN)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __builtin_nanf("");
+}
+
+// The values of a tile of 128 x 128 elements of the caller's matrix, from either image (the transposed one by way of LDS).
+template <typename E, bool COL>
+__global__ __launch_bounds__(THREADS) void k_mx_dequantize(MxMats m) {
+  constexpr int LDT = TILE + 8 / sizeof(E);
+  __shared__ E tile[COL ? TILE * LDT : 1];
+  const int t = threadIdx.x, which = blockIdx.y;
+  const int64_t tiles_c = (m.cols + TILE - 1) / TILE;
+  const int64_t r0 = blockIdx.x / tiles_c * TILE, c0 = blockIdx.x % tiles_c * TILE;
+  E* const dst = static_cast<E*>(m.mat[which]);
+  if constexpr (COL) {
+    const uint8_t* const img = m.by_col[which];
+    const int64_t units = mx_k_units(m.rows), ks = r0 / MX_UNIT_K;
+    const int c = t & (TILE - 1);
+    const int64_t rt = (c0 + c) / MX_UNIT_ROWS;
+    if (c0 + c < m.cols) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int rb = (t >> 7) + 2 * i;
+        const u32x4 codes = *reinterpret_cast<const u32x4*>(img + (rt * units + ks) * MX_UNIT_BYTES + (rb * 16 + c % 16) * 16);
+        const unsigned byte = img[mx_code_bytes(m.cols, m.rows) + (rt / 4 * units + ks) * MX_SCALE_BYTES + (rb * 16 + c % 16) * 4 + rt % 4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          float v[8];
+          eight_values(codes[q], byte, v);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) tile[(rb * MX_BLOCK + q * 8 + e) * LDT + c] = static_cast<E>(v[e]);
+        }
+      }
+    }
+    __syncthreads();
+  }
+  const int col = (t & 15) * 8;
+  const int64_t left = m.cols - (c0 + col);
+  if (left <= 0) return;
+#pragma unroll 4
+  for (int i = 0; i < TILE / 16; ++i) {
+    const int row = i * 16 + (t >> 4);
+    if (r0 + row >= m.rows) break;
+    float v[8];
+    if constexpr (COL) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(tile[row * LDT + col + e]);
+    } else {
+      const uint8_t* const img = m.by_row[which];
+      const int64_t units = mx_k_units(m.cols), ks = c0 / MX_UNIT_K, rt = (r0 + row) / MX_UNIT_ROWS;
+      const int at = ((t & 15) >> 2) * 16 + row % 16;
+      const unsigned codes = *reinterpret_cast<const unsigned*>(img + (rt * units + ks) * MX_UNIT_BYTES + at * 16 + (t & 3) * 4);
+      const unsigned byte = img[mx_code_bytes(m.rows, m.cols) + (rt / 4 * units + ks) * MX_SCALE_BYTES + at * 4 + rt % 4];
+      eight_values(codes, byte, v);
+    }
+    store8(dst + (r0 + row) * m.ld + c0 + col, left, v);
+  }
+}
+
+dim3 tiles_of(const MxMats& m) {
+  return dim3(static_cast<unsigned>((m.rows + TILE - 1) / TILE * ((m.cols + TILE - 1) / TILE)), static_cast<unsigned>(m.n));
+}
+
+template <typename E, bool NOISE>
+void quantize_sides(const MxMats& m, hipStream_t st) {
+  if (m.by_row[0] && m.by_col[0])
+    k_mx_quantize<E, true, true, NOISE><<<tiles_of(m), THREADS, 0, st>>>(m);
+  else if (m.by_row[0])
+    k_mx_quantize<E, true, false, NOISE><<<tiles_of(m), THREADS, 0, st>>>(m);
+  else
+    k_mx_quantize<E, false, true, NOISE><<<tiles_of(m), THREADS, 0, st>>>(m);
+}
+
+}  // namespace
+
+hipError_t launch_mx_quantize(const MxMats& m, hipStream_t st) {
+  if (m.dtype == CANZ_DT_F32)
+    m.noise[0] ? quantize_sides<float, true>(m, st) : quantize_sides<float, false>(m, st);
+  else
+    m.noise[0] ? quantize_sides<__bf16, true>(m, st) : quantize_sides<__bf16, false>(m, st);
+  return hipGetLastError();
+}
+
+hipError_t launch_mx_dequantize(const MxMats& m, hipStream_t st) {
+  const bool col = m.by_col[0] != nullptr;
+  if (m.dtype == CANZ_DT_F32)
+    col ? k_mx_dequantize<float, true><<<tiles_of(m), THREADS, 0, st>>>(m) : k_mx_dequantize<float, false><<<tiles_of(m), THREADS, 0, st>>>(m);
+  else
+    col ? k_mx_dequantize<__bf16, true><<<tiles_of(m), THREADS, 0, st>>>(m) : k_mx_dequantize<__bf16, false><<<tiles_of(m), THREADS, 0, st>>>(m);
+  return hipGetLastError();
+}
+
+}  // namespace canz

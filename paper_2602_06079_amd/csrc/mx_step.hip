@@ -1,0 +1,238 @@
+// canz_mx_*: host side of the microscaled images and their products.  Validates the groups and enqueues the launches on the caller's
+// stream; nothing here allocates, copies to the device or synchronises.
+#include <algorithm>
+
+#include "canz_internal.h"
+#include "kernels.h"
+#include "mx.h"
+
+namespace canz {
+
+int check_mx_group(const canz_mx_group& g, int idx, bool back) {
+  if (g.n_mats < 0) return fail(CANZ_EINVAL, "group %d: n_mats < 0", idx);
+  if (g.rows < 0 || g.cols < 0) return fail(CANZ_EINVAL, "group %d: negative extent", idx);
+  if (g.rows > MX_MAX_EXTENT || g.cols > MX_MAX_EXTENT)
+    return fail(CANZ_ESHAPE, "group %d: extent above %lld", idx, static_cast<long long>(MX_MAX_EXTENT));
+  if (!mx_fits_grid(g.rows, g.cols)) return fail(CANZ_ESHAPE, "group %d: more than 2^37 padded elements in a matrix", idx);
+  if (g.dtype != CANZ_DT_F32 && g.dtype != CANZ_DT_BF16) return fail(CANZ_EUNSUPPORTED, "group %d: unknown dtype", idx);
+  if (g.ld < g.cols) return fail(CANZ_EINVAL, "group %d: ld below cols", idx);
+  if (g.n_mats == 0 || g.rows == 0 || g.cols == 0) return CANZ_OK;
+  if (!g.mat) return fail(CANZ_EINVAL, "group %d: null pointer table", idx);
+  if (!g.by_row && !g.by_col) return fail(CANZ_EINVAL, "group %d: neither by_row nor by_col", idx);
+  if (back && g.by_row && g.by_col) return fail(CANZ_EINVAL, "group %d: one of by_row and by_col is read, both are given", idx);
+  auto bad = [](const void* p, uintptr_t align) { return p == nullptr || (reinterpret_cast<uintptr_t>(p) & (align - 1)) != 0; };
+  for (int i = 0; i < g.n_mats; ++i) {
+    if (bad(g.mat[i], 16)) return fail(CANZ_EINVAL, "group %d: mat[%d] null or not 16-byte aligned", idx, i);
+    if (g.by_row && bad(g.by_row[i], 256)) return fail(CANZ_EINVAL, "group %d: by_row[%d] null or not 256-byte aligned", idx, i);
+    if (g.by_col && bad(g.by_col[i], 256)) return fail(CANZ_EINVAL, "group %d: by_col[%d] null or not 256-byte aligned", idx, i);
+    if (!back && g.noise && g.noise[i] == nullptr) return fail(CANZ_EINVAL, "group %d: noise[%d] null", idx, i);
+  }
+  return CANZ_OK;
+}
+
+namespace {
+
+constexpr size_t ALIGN = 256;
+
+// calls fn(MxMats) for every launch of a checked group
+template <typename F>
+int for_each_launch(const canz_mx_group& g, int scale_mode, bool noise, F&& fn) {
+  if (g.rows == 0 || g.cols == 0) return CANZ_OK;
+  for (int first = 0; first < g.n_mats; first += MX_MAX_MATS) {
+    MxMats m{};
+    m.rows = g.rows, m.cols = g.cols, m.ld = g.ld;
+    m.n = std::min(MX_MAX_MATS, g.n_mats - first);
+    m.dtype = g.dtype, m.scale_mode = scale_mode;
+    for (int i = 0; i < m.n; ++i) {
+      m.mat[i] = g.mat[first + i];
+      m.by_row[i] = g.by_row ? static_cast<uint8_t*>(g.by_row[first + i]) : nullptr;
+      m.by_col[i] = g.by_col ? static_cast<uint8_t*>(g.by_col[first + i]) : nullptr;
+      m.noise[i] = noise && g.noise ? static_cast<const uint8_t*>(g.noise[first + i]) : nullptr;
+    }
+    const hipError_t err = fn(m);
+    if (err != hipSuccess) return fail(CANZ_EHIP, "microscaled image: %s", hipGetErrorString(err));
+  }
+  return CANZ_OK;
+}
+
+int check_scale_mode(int32_t mode) {
+  if (mode != CANZ_MX_SCALE_FLOOR && mode != CANZ_MX_SCALE_CEIL) return fail(CANZ_EUNSUPPORTED, "unknown scale_mode %d", mode);
+  return CANZ_OK;
+}
+
+bool mx_idle(const canz_mx_product_group& g) { return g.n_prods == 0 || g.m == 0 || g.n == 0; }
+
+int check_product_group(const canz_mx_product_group& g, int idx, bool need_ptrs) {
+  if (g.n_prods < 0) return fail(CANZ_EINVAL, "group %d: n_prods < 0", idx);
+  if (g.m < 0 || g.n < 0 || g.k < 0) return fail(CANZ_EINVAL, "group %d: negative extent", idx);
+  if (g.m > MX_MAX_EXTENT || g.n > MX_MAX_EXTENT || g.k > MX_MAX_EXTENT)
+    return fail(CANZ_ESHAPE, "group %d: extent above %lld", idx, static_cast<long long>(MX_MAX_EXTENT));
+  if (!mx_fits_grid(g.m, g.n) || !mx_fits_grid(g.m, g.k) || !mx_fits_grid(g.n, g.k))
+    return fail(CANZ_ESHAPE, "group %d: more than 2^37 padded elements in a matrix", idx);
+  if (g.a_dtype != CANZ_DT_F32 && g.a_dtype != CANZ_DT_BF16 && g.a_dtype != CANZ_DT_MX)
+    return fail(CANZ_EUNSUPPORTED, "group %d: unknown a_dtype", idx);
+  if (g.out_dtype != CANZ_DT_F32 && g.out_dtype != CANZ_DT_BF16) return fail(CANZ_EUNSUPPORTED, "group %d: unknown out_dtype", idx);
+  if (int rc = check_scale_mode(g.a_scale_mode)) return rc;
+  if (g.a_dtype != CANZ_DT_MX && g.lda < g.k) return fail(CANZ_EINVAL, "group %d: lda below k", idx);
+  if (g.ldc < g.n) return fail(CANZ_EINVAL, "group %d: ldc below n", idx);
+  if (!need_ptrs || mx_idle(g)) return CANZ_OK;
+  if (!g.c || (g.k > 0 && (!g.a || !g.b))) return fail(CANZ_EINVAL, "group %d: null pointer table", idx);
+  auto bad = [](const void* p, uintptr_t align) { return p == nullptr || (reinterpret_cast<uintptr_t>(p) & (align - 1)) != 0; };
+  for (int i = 0; i < g.n_prods; ++i) {
+    if (bad(g.c[i], 16)) return fail(CANZ_EINVAL, "group %d: c[%d] null or not 16-byte aligned", idx, i);
+    if (g.k == 0) continue;
+    const bool image = g.a_dtype == CANZ_DT_MX;
+    if (bad(g.a[i], image ? 256 : 16)) return fail(CANZ_EINVAL, "group %d: a[%d] null or not %d-byte aligned", idx, i, image ? 256 : 16);
+    if (bad(g.b[i], 256)) return fail(CANZ_EINVAL, "group %d: b[%d] null or not 256-byte aligned", idx, i);
+  }
+  return CANZ_OK;
+}
+
+// room for the image of every A that the call rounds itself
+size_t product_workspace(const canz_mx_product_group* g, int32_t n_groups) {
+  size_t need = 0;
+  for (int i = 0; i < n_groups; ++i)
+    if (!mx_idle(g[i]) && g[i].a_dtype != CANZ_DT_MX) need += static_cast<size_t>(g[i].n_prods) * mx_image_bytes(g[i].m, g[i].k);
+  return std::max(need, ALIGN);
+}
+
+}  // namespace
+
+int quantize_group(const canz_mx_group& g, int scale_mode, hipStream_t st) {
+  return for_each_launch(g, scale_mode, true, [&](const MxMats& m) { return launch_mx_quantize(m, st); });
+}
+
+}  // namespace canz
+
+extern "C" int canz_mx_image_bytes(int64_t rows, int64_t cols, size_t* bytes_out) {
+  using namespace canz;
+  if (!bytes_out) return fail(CANZ_EINVAL, "null output pointer");
+  if (rows < 0 || cols < 0) return fail(CANZ_EINVAL, "negative extent");
+  if (rows > MX_MAX_EXTENT || cols > MX_MAX_EXTENT) return fail(CANZ_ESHAPE, "extent above %lld", static_cast<long long>(MX_MAX_EXTENT));
+  *bytes_out = static_cast<size_t>(mx_image_bytes(rows, cols));
+  return CANZ_OK;
+}
+
+extern "C" int canz_mx_quantize(const canz_mx_group* g, int32_t n_groups, int32_t scale_mode, void* hip_stream) {
+  using namespace canz;
+  if (n_groups < 0 || (n_groups > 0 && !g)) return fail(CANZ_EINVAL, "bad group array");
+  if (int rc = check_scale_mode(scale_mode)) return rc;
+  for (int i = 0; i < n_groups; ++i)
+    if (int rc = check_mx_group(g[i], i, false)) return rc;
+  const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  const StreamDevice on(st);
+  if (on.error() != hipSuccess) return fail(CANZ_EHIP, "stream: %s", hipGetErrorString(on.error()));
+  for (int i = 0; i < n_groups; ++i)
+    if (int rc = quantize_group(g[i], scale_mode, st)) return rc;
+  return CANZ_OK;
+}
+
+extern "C" int canz_mx_dequantize(const canz_mx_group* g, int32_t n_groups, void* hip_stream) {
+  using namespace canz;
+  if (n_groups < 0 || (n_groups > 0 && !g)) return fail(CANZ_EINVAL, "bad group array");
+  for (int i = 0; i < n_groups; ++i)
+    if (int rc = check_mx_group(g[i], i, true)) return rc;
+  const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  const StreamDevice on(st);
+  if (on.error() != hipSuccess) return fail(CANZ_EHIP, "stream: %s", hipGetErrorString(on.error()));
+  for (int i = 0; i < n_groups; ++i) {
+    const int rc = for_each_launch(g[i], 0, false, [&](const MxMats& m) { return launch_mx_dequantize(m, st); });
+    if (rc) return rc;
+  }
+  return CANZ_OK;
+}
+
+extern "C" int canz_mx_product_workspace_bytes(const canz_mx_product_group* g, int32_t n_groups, size_t* bytes_out) {
+  using namespace canz;
+  if (!bytes_out) return fail(CANZ_EINVAL, "null output pointer");
+  if (n_groups < 0 || (n_groups > 0 && !g)) return fail(CANZ_EINVAL, "bad group array");
+  for (int i = 0; i < n_groups; ++i)
+    if (int rc = check_product_group(g[i], i, false)) return rc;
+  *bytes_out = product_workspace(g, n_groups);
+  return CANZ_OK;
+}
+
+extern "C" int canz_mx_product(const canz_mx_product_group* g, int32_t n_groups, void* workspace, size_t workspace_bytes,
+                               void* hip_stream) {
+  using namespace canz;
+  if (n_groups < 0 || (n_groups > 0 && !g)) return fail(CANZ_EINVAL, "bad group array");
+  bool any = false;
+  for (int i = 0; i < n_groups; ++i) {
+    if (int rc = check_product_group(g[i], i, true)) return rc;
+    any = any || !mx_idle(g[i]);
+  }
+  if (!any) return CANZ_OK;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & (ALIGN - 1)))
+    return fail(CANZ_EWORKSPACE, "workspace null or not 256-byte aligned");
+  const size_t need = product_workspace(g, n_groups);
+  if (workspace_bytes < need) return fail(CANZ_EWORKSPACE, "workspace too small: %zu bytes given, %zu needed", workspace_bytes, need);
+  const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  const StreamDevice on(st);
+  if (on.error() != hipSuccess) return fail(CANZ_EHIP, "stream: %s", hipGetErrorString(on.error()));
+
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  MxProblems ps;
+  ps.n = 0;
+  auto flush = [&]() {
+    const hipError_t err = launch_mx_product(ps, st);
+    ps.n = 0;
+    return err == hipSuccess ? CANZ_OK : fail(CANZ_EHIP, "microscaled product: %s", hipGetErrorString(err));
+  };
+  for (int i = 0; i < n_groups; ++i) {
+    const canz_mx_product_group& gi = g[i];
+    if (mx_idle(gi)) continue;
+    uint8_t* const images = ws;
+    const size_t each = static_cast<size_t>(mx_image_bytes(gi.m, gi.k));
+    if (gi.a_dtype != CANZ_DT_MX && gi.k > 0) {
+      for (int first = 0; first < gi.n_prods; first += MX_MAX_MATS) {
+        MxMats m{};
+        m.rows = gi.m, m.cols = gi.k, m.ld = gi.lda;
+        m.n = std::min(MX_MAX_MATS, gi.n_prods - first);
+        m.dtype = gi.a_dtype, m.scale_mode = gi.a_scale_mode;
+        for (int x = 0; x < m.n; ++x) {
+          m.mat[x] = const_cast<void*>(gi.a[first + x]);
+          m.by_row[x] = images + (first + x) * each;
+        }
+        const hipError_t err = launch_mx_quantize(m, st);
+        if (err != hipSuccess) return fail(CANZ_EHIP, "microscaled product: %s", hipGetErrorString(err));
+      }
+      ws += gi.n_prods * each;
+    }
+    for (int x = 0; x < gi.n_prods; ++x) {
+      MxProblem& p = ps.pr[ps.n++];
+      p.a = gi.a_dtype == CANZ_DT_MX ? static_cast<const uint8_t*>(gi.k > 0 ? gi.a[x] : nullptr) : images + x * each;
+      p.b = static_cast<const uint8_t*>(gi.k > 0 ? gi.b[x] : nullptr);
+      p.c = gi.c[x];
+      p.m = gi.m, p.n = gi.n, p.k = gi.k, p.ldc = gi.ldc;
+      p.alpha = gi.alpha, p.beta = gi.beta, p.out_dtype = gi.out_dtype;
+      if (ps.n == MX_MAX_PROBLEMS)
+        if (int rc = flush()) return rc;
+    }
+  }
+  return ps.n > 0 ? flush() : CANZ_OK;
+}
+
+extern "C" int canz_muon_step_images(const canz_group* g, int32_t n_groups, const canz_muon_hparams* hp, const canz_mx_images* images,
+                                     int32_t scale_mode, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  using namespace canz;
+  if (n_groups < 0 || (n_groups > 0 && (!g || !images))) return fail(CANZ_EINVAL, "bad group array");
+  if (!hp) return fail(CANZ_EINVAL, "null hparams");
+  if (hp->out_mode != CANZ_OUT_PARAM) return fail(CANZ_EUNSUPPORTED, "images are taken of updated parameters: out_mode must be CANZ_OUT_PARAM");
+  if (int rc = check_scale_mode(scale_mode)) return rc;
+  const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  // everything is checked before the step is enqueued; the second time round the images are
+  for (int pass = 0; pass < 2; ++pass) {
+    for (int i = 0; i < n_groups; ++i) {
+      if (!images[i].by_row && !images[i].by_col) continue;
+      canz_mx_group m{};
+      m.rows = g[i].rows, m.cols = g[i].cols, m.ld = g[i].cols;
+      m.n_mats = g[i].n_mats, m.dtype = g[i].out_dtype;
+      m.mat = g[i].out, m.by_row = images[i].by_row, m.by_col = images[i].by_col;
+      const int rc = pass == 0 ? check_mx_group(m, i, false) : quantize_group(m, scale_mode, st);
+      if (rc) return rc;
+    }
+    if (pass == 1) return CANZ_OK;
+    if (int rc = canz_muon_step(g, n_groups, hp, workspace, workspace_bytes, hip_stream)) return rc;
+  }
+  return CANZ_OK;
+}
