@@ -76,15 +76,15 @@ def image_bytes(rows: int, cols: int) -> int:
 
 
 def unpack(image: np.ndarray, rows: int, cols: int):
-    """(codes, scales, everything else is zero) of an image's bytes, by the layout of include/canz.h: units of 16 x 128 codes and of
-    64 x 128 scales."""
+    """(codes, scales, everything else is zero) of an image's bytes: units of 16 rows x 128 columns of codes and of 64 x 128 of scales; two
+    units of codes share 32 rows, four rows of one, then four of the other."""
     r, k = -(-rows // 64) * 64, -(-cols // 128) * 128
     n = r * k // 2
-    # codes: [row tile][k unit][block][row][byte]
-    c = image[:n].reshape(r // 16, k // 128, 4, 16, 16).transpose(0, 3, 1, 2, 4).reshape(r, k // 2)
+    # codes: [32 rows][unit][k unit][block][piece of four rows][row][byte]
+    c = image[:n].reshape(r // 32, 2, k // 128, 4, 4, 4, 16).transpose(0, 4, 1, 5, 2, 3, 6).reshape(r, k // 2)
     codes = np.stack([c & 15, c >> 4], axis=-1).reshape(r, k)
-    # scales: [64 rows][k unit][block][row][row tile]
-    s = image[n:].reshape(r // 64, k // 128, 4, 16, 4).transpose(0, 4, 3, 1, 2).reshape(r, k // 32)
+    # scales: [64 rows][k unit][block][piece][row][32 rows][unit]
+    s = image[n:].reshape(r // 64, k // 128, 4, 4, 4, 2, 2).transpose(0, 5, 3, 6, 4, 1, 2).reshape(r, k // 32)
     nb = -(-cols // BLOCK)
     clean = not codes[rows:].any() and not codes[:, cols:].any() and not s[rows:].any() and not s[:, nb:].any()
     return codes[:rows, :cols], s[:rows, :nb], clean
@@ -98,8 +98,8 @@ def pack(codes: np.ndarray, scales: np.ndarray) -> np.ndarray:
     c[:rows, :cols] = codes
     s = np.zeros((r, k // 32), dtype=np.uint8)
     s[:rows, :scales.shape[1]] = scales
-    c = (c[:, 0::2] | c[:, 1::2] << 4).reshape(r // 16, 16, k // 128, 4, 16).transpose(0, 2, 3, 1, 4)
-    s = s.reshape(r // 64, 4, 16, k // 128, 4).transpose(0, 3, 4, 2, 1)
+    c = (c[:, 0::2] | c[:, 1::2] << 4).reshape(r // 32, 4, 2, 4, k // 128, 4, 16).transpose(0, 2, 4, 5, 1, 3, 6)
+    s = s.reshape(r // 64, 2, 4, 2, 4, k // 128, 4).transpose(0, 5, 6, 2, 4, 1, 3)
     return np.concatenate([c.reshape(-1), s.reshape(-1)])
 
 

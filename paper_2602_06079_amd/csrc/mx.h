@@ -56,9 +56,10 @@ struct MxProblem {
 constexpr int MX_MAX_PROBLEMS = 32;
 struct MxProblems {
   int n;
+  int tiles;        // of all problems, set by the launcher
   MxProblem pr[MX_MAX_PROBLEMS];
 };
-hipError_t launch_mx_product(MxProblems& p, hipStream_t st);
+hipError_t launch_mx_product(const MxProblems& p, hipStream_t st);
 
 // Validates one group of canz_mx_quantize (`back`: of canz_mx_dequantize).
 int check_mx_group(const canz_mx_group& g, int idx, bool back);

@@ -142,17 +142,17 @@ __global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {
       const unsigned byte = scale_byte(amax, ceil);
       const unsigned codes = eight_codes<NOISE>(v, byte, u);
       const int kb = (t & 15) >> 2;
-      const int64_t rt = (r0 + row) / MX_UNIT_ROWS;
-      if (rt < mx_row_tiles(m.rows))
-        *reinterpret_cast<unsigned*>(m.by_row[which] + (rt * units_row + c0 / MX_UNIT_K) * MX_UNIT_BYTES + (kb * 16 + row % 16) * 16 +
+      const int64_t unit = mx_unit(r0 + row);
+      if (unit < mx_row_tiles(m.rows))
+        *reinterpret_cast<unsigned*>(m.by_row[which] + (unit * units_row + c0 / MX_UNIT_K) * MX_UNIT_BYTES + (kb * 16 + mx_slot(row)) * 16 +
                                      (t & 3) * 4) = codes;
-      if ((t & 3) == 0) reinterpret_cast<uint8_t*>(scales[0][row >> 6])[(kb * 16 + row % 16) * 4 + (row >> 4) % 4] = static_cast<uint8_t>(byte);
+      if ((t & 3) == 0) reinterpret_cast<uint8_t*>(scales[0][row >> 6])[(kb * 16 + mx_slot(row)) * 4 + mx_unit(row) % 4] = static_cast<uint8_t>(byte);
     }
   }
   __syncthreads();
   if constexpr (COL) {
     const int c = t & (TILE - 1);
-    const int64_t rt = (c0 + c) / MX_UNIT_ROWS;
+    const int64_t unit = mx_unit(c0 + c);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int rb = (t >> 7) + 2 * i;
@@ -173,9 +173,9 @@ __global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {
         }
         codes[q] = eight_codes<NOISE>(v, byte, u);
       }
-      if (rt < mx_row_tiles(m.cols))
-        *reinterpret_cast<u32x4*>(m.by_col[which] + (rt * units_col + r0 / MX_UNIT_K) * MX_UNIT_BYTES + (rb * 16 + c % 16) * 16) = codes;
-      reinterpret_cast<uint8_t*>(scales[1][c >> 6])[(rb * 16 + c % 16) * 4 + (c >> 4) % 4] = static_cast<uint8_t>(byte);
+      if (unit < mx_row_tiles(m.cols))
+        *reinterpret_cast<u32x4*>(m.by_col[which] + (unit * units_col + r0 / MX_UNIT_K) * MX_UNIT_BYTES + (rb * 16 + mx_slot(c)) * 16) = codes;
+      reinterpret_cast<uint8_t*>(scales[1][c >> 6])[(rb * 16 + mx_slot(c)) * 4 + mx_unit(c) % 4] = static_cast<uint8_t>(byte);
     }
     __syncthreads();
   }
@@ -211,13 +211,13 @@ __global__ __launch_bounds__(THREADS) void k_mx_dequantize(MxMats m) {
     const uint8_t* const img = m.by_col[which];
     const int64_t units = mx_k_units(m.rows), ks = r0 / MX_UNIT_K;
     const int c = t & (TILE - 1);
-    const int64_t rt = (c0 + c) / MX_UNIT_ROWS;
+    const int64_t unit = mx_unit(c0 + c);
     if (c0 + c < m.cols) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int rb = (t >> 7) + 2 * i;
-        const u32x4 codes = *reinterpret_cast<const u32x4*>(img + (rt * units + ks) * MX_UNIT_BYTES + (rb * 16 + c % 16) * 16);
-        const unsigned byte = img[mx_code_bytes(m.cols, m.rows) + (rt / 4 * units + ks) * MX_SCALE_BYTES + (rb * 16 + c % 16) * 4 + rt % 4];
+        const u32x4 codes = *reinterpret_cast<const u32x4*>(img + (unit * units + ks) * MX_UNIT_BYTES + (rb * 16 + mx_slot(c)) * 16);
+        const unsigned byte = img[mx_code_bytes(m.cols, m.rows) + (unit / 4 * units + ks) * MX_SCALE_BYTES + (rb * 16 + mx_slot(c)) * 4 + unit % 4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           float v[8];
@@ -242,10 +242,10 @@ __global__ __launch_bounds__(THREADS) void k_mx_dequantize(MxMats m) {
       for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(tile[row * LDT + col + e]);
     } else {
       const uint8_t* const img = m.by_row[which];
-      const int64_t units = mx_k_units(m.cols), ks = c0 / MX_UNIT_K, rt = (r0 + row) / MX_UNIT_ROWS;
-      const int at = ((t & 15) >> 2) * 16 + row % 16;
-      const unsigned codes = *reinterpret_cast<const unsigned*>(img + (rt * units + ks) * MX_UNIT_BYTES + at * 16 + (t & 3) * 4);
-      const unsigned byte = img[mx_code_bytes(m.rows, m.cols) + (rt / 4 * units + ks) * MX_SCALE_BYTES + at * 4 + rt % 4];
+      const int64_t units = mx_k_units(m.cols), ks = c0 / MX_UNIT_K, unit = mx_unit(r0 + row);
+      const int at = ((t & 15) >> 2) * 16 + mx_slot(row);
+      const unsigned codes = *reinterpret_cast<const unsigned*>(img + (unit * units + ks) * MX_UNIT_BYTES + at * 16 + (t & 3) * 4);
+      const unsigned byte = img[mx_code_bytes(m.rows, m.cols) + (unit / 4 * units + ks) * MX_SCALE_BYTES + at * 4 + unit % 4];
       eight_values(codes, byte, v);
     }
     store8(dst + (r0 + row) * m.ld + c0 + col, left, v);

@@ -117,15 +117,19 @@ def pin_layout():
     scales[67, 6] = 77
     img = mx().pack(codes, scales)
     ks = 3
-    unit = (67 // 16) * ks + 1
-    assert img[unit * 1024 + (2 * 16 + 67 % 16) * 16 + 5 // 2] == 9 << 4
-    assert img[128 * 384 // 2 + ((67 // 64) * ks + 1) * 256 + (2 * 16 + 67 % 16) * 4 + (67 // 16) % 4] == 77
+    # row 67 = 64 + 3: slot 3 of the first unit of the third 32 rows
+    assert img[(4 * ks + 1) * 1024 + (2 * 16 + 3) * 16 + 5 // 2] == 9 << 4
+    assert img[128 * 384 // 2 + (1 * ks + 1) * 256 + (2 * 16 + 3) * 4 + 0] == 77
     assert np.count_nonzero(img) == 2
+    codes[:], scales[:] = 0, 0
+    codes[46, 0], scales[46, 0] = 3, 55             # row 46 = 32 + 8 + 4 + 2: slot 4 + 2 of the second unit of the second 32 rows
+    other = mx().pack(codes, scales)
+    assert other[3 * ks * 1024 + 6 * 16] == 3 and other[128 * 384 // 2 + 6 * 4 + 3] == 55 and np.count_nonzero(other) == 2
     img[3] = 1      # row 0, k 6: not the padding
     assert mx().unpack(img, 70, 300)[2]
-    for row, block in ((127, 0), (0, 11)):      # scales of a padding row and of a padding block
+    for row64, block, slot, unit in ((1, 0, 15, 3), (0, 11, 0, 0)):      # scales of row 127 and of a padding block
         bad = img.copy()
-        bad[128 * 384 // 2 + ((row // 64) * ks + block // 4) * 256 + (block % 4 * 16 + row % 16) * 4 + (row // 16) % 4] = 1
+        bad[128 * 384 // 2 + (row64 * ks + block // 4) * 256 + (block % 4 * 16 + slot) * 4 + unit] = 1
         assert not mx().unpack(bad, 70, 300)[2]
 
 
@@ -164,7 +168,7 @@ MUTANTS = [
     ("np.exp2(scales.astype(np.float64) - 127)", "np.exp2(scales.astype(np.float64) - 126)"),
     ("np.stack([c & 15, c >> 4], axis=-1)", "np.stack([c >> 4, c & 15], axis=-1)"),
     ("c[:, 0::2] | c[:, 1::2] << 4", "c[:, 1::2] | c[:, 0::2] << 4"),
-    ("transpose(0, 4, 3, 1, 2)", "transpose(0, 3, 4, 1, 2)"),
+    ("transpose(0, 5, 3, 6, 4, 1, 2)", "transpose(0, 5, 3, 4, 6, 1, 2)"),
     ("not s[rows:].any()", "True"),
     ("return r if beta == 0.0 else r + beta * c", "return r + beta * c if c is not None else r"),
     ("alpha * (a @ b.T)", "a @ b.T"),
