@@ -44,13 +44,17 @@ struct MxMats {
 hipError_t launch_mx_quantize(const MxMats& m, hipStream_t st);
 hipError_t launch_mx_dequantize(const MxMats& m, hipStream_t st);
 
-// C = alpha A B^T + beta C of images A (m x k) and B (n x k), several products in one launch.
+// C = alpha A B^T + beta C of images A (m x k) and B (n x k), several products in one launch.  A may also be a matrix, which the kernel rounds on
+// its way: with up to 16 rows, as long as every block rounding it again costs less than a launch that makes its image (4 us): 8 x 25600 x
+// 5120 18.4 us and 16.9 + 4, 16 x 25600 x 5120 22.7 and 15.2 + 4.5, 8 x 5120 x 25600 24.8 and 20.8 + 4.5, 8 x 4096 x 4096 5.9 and 4.5 + 4.
+constexpr bool mx_rounds_on_the_way(int64_t m, int64_t n, int64_t k) { return m <= 16 && m * n <= (int64_t(1) << 30) / (k > 0 ? k : 1); }
 struct MxProblem {
-  const uint8_t *a, *b;
+  const uint8_t* a;   // image, or the matrix's first element
+  const uint8_t* b;
   void* c;
-  int64_t m, n, k, ldc;
+  int64_t m, n, k, lda, ldc;
   float alpha, beta;
-  int out_dtype;
+  int a_dtype, a_ceil, out_dtype;
   int first_tile;   // set by the launcher
 };
 constexpr int MX_MAX_PROBLEMS = 32;

@@ -1,34 +1,21 @@
 // Microscaled 4-bit images of matrices: canz_mx_quantize and canz_mx_dequantize.
 //
 // A block of 32 consecutive elements along the contracted index shares a scale X = 2^e; an element is one of 0, .5, 1, 1.5, 2, 3, 4,
-// 6 times X.  X follows from the largest magnitude's bits: with biased exponent E the floor rule takes E - 2, the ceil rule one more
-// where the mantissa is above 1.5, neither less than 0 (2^-127).  Division by X is exact, and the conversion instruction rounds to the
-// nearest value, ties to the even code, at most 6 (v_cvt_scalef32_pk_fp4_f32; it reads the exponent field of its scale alone, so that byte << 23 is
-// 2^(byte - 127) for every byte).  The ceil rule's X stops at 2^125, where the floor rule's ends by itself.
+// 6 times X (mx_round.h).
 #include "device_util.h"
 #include "mx.h"
+#include "mx_round.h"
 
 namespace canz {
 namespace {
 
 constexpr int TILE = 128;      // rows and columns of a block's tile: whole units of codes and of scales for either image
 constexpr int THREADS = 256;
-constexpr unsigned NONFINITE = 0x7F800000u;   // magnitudes with these bits or above are infinite or NaN
-constexpr unsigned SCALE_NAN = 255u;
-constexpr int MAX_SCALE = 252;                // 2^125: six times it is the largest value that fp32 holds
 
 typedef unsigned u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
-
-// scale byte of a block whose largest magnitude has the bits `amax`
-__device__ __forceinline__ unsigned scale_byte(unsigned amax, bool ceil) {
-  if (amax >= NONFINITE) return SCALE_NAN;
-  const int e = static_cast<int>(amax >> 23) - 2 + (ceil && (amax & 0x7FFFFFu) > 0x400000u ? 1 : 0);
-  return static_cast<unsigned>(min(max(e, 0), MAX_SCALE));
-}
-__device__ __forceinline__ float scale_value(unsigned byte) { return __builtin_bit_cast(float, byte << 23); }
 
 // Code of one element with noise u in 0 .. 255: s floor((rint(256 a / s) + u) / 256) for a = |v| / X and the distance s of the values
 // around it.  Every step before the rint is exact, and it and the sum are integers below 2^11.
@@ -42,13 +29,13 @@ __device__ __forceinline__ unsigned noisy_code(float v, unsigned byte, unsigned 
 // eight codes of one block, element 0 in the lowest bits
 template <bool NOISE>
 __device__ __forceinline__ unsigned eight_codes(const float (&v)[8], unsigned byte, unsigned long long noise) {
-  if (byte == SCALE_NAN) return 0;
+  if (byte == MX_SCALE_NAN) return 0;
   unsigned r = 0;
   if constexpr (NOISE) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) r |= noisy_code(v[i], byte, static_cast<unsigned>(noise >> (8 * i)) & 255u) << (4 * i);
   } else {
-    const float s = scale_value(byte);
+    const float s = mx_scale_value(byte);
     r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[0], v[1], s, 0);
     r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[2], v[3], s, 1);
     r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[4], v[5], s, 2);
@@ -56,7 +43,6 @@ __device__ __forceinline__ unsigned eight_codes(const float (&v)[8], unsigned by
   }
   return r;
 }
-__device__ __forceinline__ unsigned magnitude(float v) { return __builtin_bit_cast(unsigned, v) & 0x7FFFFFFFu; }
 
 // eight consecutive elements of a row, those behind its end as zeros
 template <typename E>
@@ -116,7 +102,7 @@ __global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {
   const int64_t r0 = blockIdx.x / tiles_c * TILE, c0 = blockIdx.x % tiles_c * TILE;
   const E* const src = static_cast<const E*>(m.mat[which]);
   const uint8_t* const noise = NOISE ? m.noise[which] : nullptr;
-  const bool ceil = m.scale_mode == CANZ_MX_SCALE_CEIL;
+  const int ceil = m.scale_mode == CANZ_MX_SCALE_CEIL;
   const int64_t units_row = mx_k_units(m.cols), units_col = mx_k_units(m.rows);   // k units of the two images
 
   const int col = (t & 15) * 8;
@@ -136,10 +122,10 @@ __global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {
     if constexpr (ROW) {
       unsigned amax = 0;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) amax = max(amax, magnitude(v[e]));
+      for (int e = 0; e < 8; ++e) amax = max(amax, mx_magnitude(v[e]));
       amax = max(amax, static_cast<unsigned>(__shfl_xor(static_cast<int>(amax), 1, 64)));
       amax = max(amax, static_cast<unsigned>(__shfl_xor(static_cast<int>(amax), 2, 64)));
-      const unsigned byte = scale_byte(amax, ceil);
+      const unsigned byte = mx_scale_byte(amax, ceil);
       const unsigned codes = eight_codes<NOISE>(v, byte, u);
       const int kb = (t & 15) >> 2;
       const int64_t unit = mx_unit(r0 + row);
@@ -158,8 +144,8 @@ __global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {
       const int rb = (t >> 7) + 2 * i;
       unsigned amax = 0;
 #pragma unroll
-      for (int e = 0; e < MX_BLOCK; ++e) amax = max(amax, magnitude(static_cast<float>(tile[(rb * MX_BLOCK + e) * TILE + c])));
-      const unsigned byte = scale_byte(amax, ceil);
+      for (int e = 0; e < MX_BLOCK; ++e) amax = max(amax, mx_magnitude(static_cast<float>(tile[(rb * MX_BLOCK + e) * TILE + c])));
+      const unsigned byte = mx_scale_byte(amax, ceil);
       u32x4 codes;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
@@ -189,11 +175,11 @@ __global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {
 }
 
 __device__ __forceinline__ void eight_values(unsigned codes, unsigned byte, float (&v)[8]) {
-  const float s = scale_value(byte == SCALE_NAN ? 127u : byte);
+  const float s = mx_scale_value(byte == MX_SCALE_NAN ? 127u : byte);
   const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 1);
   const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 3);
   v[0] = a[0], v[1] = a[1], v[2] = b[0], v[3] = b[1], v[4] = c[0], v[5] = c[1], v[6] = d[0], v[7] = d[1];
-  if (byte == SCALE_NAN)
+  if (byte == MX_SCALE_NAN)
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = __builtin_nanf("");
 }

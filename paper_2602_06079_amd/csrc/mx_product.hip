@@ -8,6 +8,7 @@
 
 #include "device_util.h"
 #include "mx.h"
+#include "mx_round.h"
 
 namespace canz {
 namespace {
@@ -23,8 +24,8 @@ typedef float f32x8 __attribute__((ext_vector_type(8)));
 #define CANZ_INLINE __attribute__((always_inline))
 #define CANZ_FENCE() __builtin_amdgcn_sched_barrier(0)
 
-using Yes = std::true_type;
-using No = std::false_type;
+// A kernel's argument where it lies: scalar loads at any index, and no copy of it.
+typedef const __attribute__((address_space(4))) MxProblems* KernArgs;
 
 template <typename F, int... I>
 __device__ __forceinline__ void static_for(F&& f, std::integer_sequence<int, I...>) {
@@ -33,6 +34,13 @@ __device__ __forceinline__ void static_for(F&& f, std::integer_sequence<int, I..
 template <int N, typename F>
 __device__ __forceinline__ void static_for(F&& f) {
   static_for(f, std::make_integer_sequence<int, N>{});
+}
+
+// Which of the launch's pieces of work this block has: the blocks of one XCD (blockIdx % 8) are neighbours, and share what they read in its L2.
+constexpr int N_XCD = 8;
+__device__ __forceinline__ int xcd_slot() {
+  const int per = gridDim.x / N_XCD, rem = gridDim.x % N_XCD, xcd = blockIdx.x % N_XCD, q = blockIdx.x / N_XCD;
+  return xcd < rem ? xcd * (per + 1) + q : rem * (per + 1) + (xcd - rem) * per + q;
 }
 
 // acc[16 slots of p][16 slots of q] += P Q^T over 128 k; SP, SQ: which byte of its scale register belongs to the unit
@@ -78,52 +86,248 @@ __device__ __forceinline__ void store_eight(E* c, int64_t left, f32x8 v) {
   }
 }
 
-// ---- one wavefront per 32 x 32 part of C, operands straight from memory: few rows, and k = 0 -------------------------------
-constexpr int FEW = 64;   // rows and columns of a block's tile
-template <typename E, bool BETA>
-__global__ __launch_bounds__(THREADS) void k_mx_product_few(MxProblems ps) {
-  int j = 0;
-  while (j + 1 < ps.n && static_cast<int>(blockIdx.x) >= ps.pr[j + 1].first_tile) ++j;
-  const MxProblem p = ps.pr[j];
-  const int tile = blockIdx.x - p.first_tile, tiles_m = static_cast<int>((p.m + FEW - 1) / FEW);
-  const int64_t m0 = static_cast<int64_t>(tile % tiles_m) * FEW, n0 = static_cast<int64_t>(tile / tiles_m) * FEW;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t row_w = m0 + (wave >> 1) * 32, col_w = n0 + (wave & 1) * 32;
-  const int64_t ks = mx_k_units(p.k);
-  // images are padded to 64 rows, so that every unit of the tile exists
-  const uint8_t* const a = p.a + row_w / MX_UNIT_ROWS * ks * MX_UNIT_BYTES + lane * 16;
-  const uint8_t* const b = p.b + col_w / MX_UNIT_ROWS * ks * MX_UNIT_BYTES + lane * 16;
-  const uint8_t* const sa = p.a + mx_code_bytes(p.m, p.k) + m0 / MX_PAD_ROWS * ks * MX_SCALE_BYTES + lane * 4;
-  const uint8_t* const sb = p.b + mx_code_bytes(p.n, p.k) + n0 / MX_PAD_ROWS * ks * MX_SCALE_BYTES + lane * 4;
-  f32x4 acc[2][2] = {};
-  for (int64_t u = 0; u < ks; ++u) {
-    i32x4 fa[2], fb[2];
+// ---- few rows: B goes by once -------------------------------------------------------------------------------------------------
+// A block has UN units of 16 rows of B and all of k, which its wavefronts share unit by unit, so that together they read B in long pieces; A's
+// units (UM of 16 rows) are multiplied with it from registers, and the wavefronts' sums are added in LDS in their order.  Memory is all
+// that takes time, and each wavefront keeps AHEAD units in flight.
+//
+// The operand layout gives a lane 32 consecutive elements of one row, a block: a matrix A is rounded by the lane that needs it, without
+// a word to another one, so that a call of few rows is one launch.
+constexpr int FEW_ROWS = 64;
+
+// the operand of one lane: 32 elements and their scale byte
+struct Block {
+  i32x4 codes;
+  int scale;
+};
+template <typename A>
+struct RawBlock;   // 32 elements on their way from memory
+template <>
+struct RawBlock<uint8_t> {
+  i32x4 codes;
+};
+template <>
+struct RawBlock<__bf16> {
+  bf16x8_any v[4];
+};
+template <>
+struct RawBlock<float> {
+  f32x4_any v[8];
+};
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ Block round_block(const RawBlock<__bf16>& x, int ceil) {
+  u16x2 top = {0, 0};
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      fa[i] = *reinterpret_cast<const i32x4*>(a + (i * ks + u) * MX_UNIT_BYTES);
-      fb[i] = *reinterpret_cast<const i32x4*>(b + (i * ks + u) * MX_UNIT_BYTES);
+  for (int i = 0; i < 4; ++i) {
+    const i32x4 w = __builtin_bit_cast(i32x4, x.v[i]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, w[e] & 0x7FFF7FFF));
+  }
+  const unsigned byte = mx_scale_byte(static_cast<unsigned>(max(top[0], top[1])) << 16, ceil);
+  const float s = mx_scale_value(byte);
+  Block r;
+  r.scale = static_cast<int>(byte);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    unsigned c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, mx_bf16x2{x.v[i][0], x.v[i][1]}, s, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, mx_bf16x2{x.v[i][2], x.v[i][3]}, s, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, mx_bf16x2{x.v[i][4], x.v[i][5]}, s, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, mx_bf16x2{x.v[i][6], x.v[i][7]}, s, 3);
+    r.codes[i] = static_cast<int>(c);
+  }
+  return r;
+}
+__device__ __forceinline__ Block round_block(const RawBlock<float>& x, int ceil) {
+  unsigned top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) top = max(top, mx_magnitude(x.v[i][e]));
+  const unsigned byte = mx_scale_byte(top, ceil);
+  const float s = mx_scale_value(byte);
+  Block r;
+  r.scale = static_cast<int>(byte);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    unsigned c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x.v[2 * i][0], x.v[2 * i][1], s, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x.v[2 * i][2], x.v[2 * i][3], s, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x.v[2 * i + 1][0], x.v[2 * i + 1][1], s, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x.v[2 * i + 1][2], x.v[2 * i + 1][3], s, 3);
+    r.codes[i] = static_cast<int>(c);
+  }
+  return r;
+}
+
+// A: uint8_t for an image, or the type of the matrix
+template <typename A, int UM, int UN, int WAVES, int AHEAD>
+__global__ __launch_bounds__(64 * WAVES) void k_mx_product_few(MxProblems) {
+  constexpr bool IMAGE = sizeof(A) == 1;
+  const KernArgs ps = (KernArgs)__builtin_amdgcn_kernarg_segment_ptr();
+  __shared__ f32x4 sums[WAVES][UM * UN][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int slot = xcd_slot();
+  int j = 0;
+  while (j + 1 < ps->n && slot >= ps->pr[j + 1].first_tile) ++j;
+  const int64_t m = ps->pr[j].m, n = ps->pr[j].n, k = ps->pr[j].k, lda = ps->pr[j].lda;
+  const int64_t part = slot - ps->pr[j].first_tile;   // of B
+  const int ks = static_cast<int>(mx_k_units(k));
+  const uint8_t* const bc = ps->pr[j].b + part * UN * ks * MX_UNIT_BYTES + lane * 16;
+  const uint8_t* const bs = ps->pr[j].b + mx_code_bytes(n, k) + part * UN / 4 * ks * MX_SCALE_BYTES + lane * 4;
+  const int b_shift = UN == 4 ? 0 : static_cast<int>(part % (4 / UN)) * UN * 8;
+  const uint8_t* const a = ps->pr[j].a;
+  // this lane's row of every 16, at its block of unit 0, in the image or in the matrix; a row that is not there is read as the last
+  const uint8_t *codes[UM], *scales[UM];
+  int a_shift[UM];
+  const A* row[UM];
+#pragma unroll
+  for (int i = 0; i < UM; ++i) {
+    const int r = min(i * 16 + (lane & 15), static_cast<int>(m) - 1);
+    if constexpr (IMAGE) {
+      const int at = (lane >> 4) * 16 + mx_slot(r);
+      codes[i] = a + static_cast<int64_t>(mx_unit(r)) * ks * MX_UNIT_BYTES + at * 16;
+      scales[i] = a + mx_code_bytes(m, k) + at * 4;
+      a_shift[i] = mx_unit(r) * 8;
+    } else {
+      row[i] = reinterpret_cast<const A*>(a) + r * lda + (lane >> 4) * MX_BLOCK;
     }
-    // the wavefront's two units are bytes 0 and 1 or 2 and 3 of the scale registers
-    const int va = *reinterpret_cast<const int*>(sa + u * MX_SCALE_BYTES) >> (wave >> 1) * 16;
-    const int vb = *reinterpret_cast<const int*>(sb + u * MX_SCALE_BYTES) >> (wave & 1) * 16;
-    acc[0][0] = mfma<0, 0>(fb[0], fa[0], acc[0][0], vb, va);
-    acc[0][1] = mfma<1, 0>(fb[1], fa[0], acc[0][1], vb, va);
-    acc[1][0] = mfma<0, 1>(fb[0], fa[1], acc[1][0], vb, va);
-    acc[1][1] = mfma<1, 1>(fb[1], fa[1], acc[1][1], vb, va);
+  }
+  const int ceil = ps->pr[j].a_ceil;
+  f32x4 acc[UM][UN] = {};
+  RawBlock<A> ra[AHEAD][UM];
+  i32x4 rb[AHEAD][UN];
+  int rsa[AHEAD][UM], rsb[AHEAD];
+  auto load_b = [&](int d, int64_t u) CANZ_INLINE {
+#pragma unroll
+    for (int q = 0; q < UN; ++q) rb[d][q] = *reinterpret_cast<const i32x4*>(bc + (static_cast<int64_t>(q) * ks + u) * MX_UNIT_BYTES);
+    rsb[d] = *reinterpret_cast<const int*>(bs + u * MX_SCALE_BYTES);
+  };
+  auto load = [&](int d, int64_t u) CANZ_INLINE {
+    load_b(d, u);
+#pragma unroll
+    for (int i = 0; i < UM; ++i) {
+      if constexpr (IMAGE) {
+        ra[d][i].codes = *reinterpret_cast<const i32x4*>(codes[i] + u * MX_UNIT_BYTES);
+        rsa[d][i] = *reinterpret_cast<const int*>(scales[i] + u * MX_SCALE_BYTES);
+      } else {
+        constexpr int PARTS = sizeof(ra[d][i].v) / 16;
+#pragma unroll
+        for (int q = 0; q < PARTS; ++q)
+          ra[d][i].v[q] = *reinterpret_cast<const decltype(ra[d][i].v[q] + ra[d][i].v[q])*>(row[i] + u * MX_UNIT_K + q * (MX_BLOCK / PARTS));
+      }
+    }
+  };
+  // `there`: a unit that is not there was read as another one and counts nothing
+  auto multiply = [&](int d, bool there) CANZ_INLINE {
+    const int vb = rsb[d] >> b_shift;
+    static_for<UM>([&](auto x) CANZ_INLINE {
+      constexpr int i = decltype(x)::value;
+      Block b;
+      if constexpr (IMAGE)
+        b.codes = ra[d][i].codes, b.scale = rsa[d][i] >> a_shift[i];
+      else
+        b = round_block(ra[d][i], ceil);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) b.codes[e] = there ? b.codes[e] : 0;
+      static_for<UN>([&](auto y) CANZ_INLINE {
+        constexpr int q = decltype(y)::value;
+        acc[i][q] = mfma<q, 0>(rb[d][q], b.codes, acc[i][q], vb, b.scale);
+      });
+    });
+  };
+  // units that are there as a whole; the last one of a matrix may not be
+  const int whole = IMAGE ? ks : static_cast<int>(k / MX_UNIT_K);
+  if (wave < whole) {
+    const int last = whole - 1;
+#pragma unroll
+    for (int d = 0; d < AHEAD; ++d) {
+      load(d, min(wave + d * WAVES, last));
+      CANZ_FENCE();   // in this order, or the compiler has no count of the younger loads to wait with
+    }
+    int u = wave;
+#pragma clang loop unroll(disable)
+    for (; u + AHEAD * WAVES < whole; u += AHEAD * WAVES) {
+#pragma unroll
+      for (int d = 0; d < AHEAD; ++d) {
+        multiply(d, true);
+        CANZ_FENCE();
+        load(d, min(u + (AHEAD + d) * WAVES, last));
+        CANZ_FENCE();
+      }
+    }
+#pragma unroll
+    for (int d = 0; d < AHEAD; ++d) {
+      multiply(d, u + d * WAVES < whole);
+      CANZ_FENCE();
+    }
+  }
+  if (!IMAGE && whole < ks && wave == whole % WAVES) {
+    load_b(0, whole);
+    const int64_t left = k - static_cast<int64_t>(whole) * MX_UNIT_K - (lane >> 4) * MX_BLOCK;   // of this lane's block
+#pragma unroll
+    for (int i = 0; i < UM; ++i) {
+      if constexpr (!IMAGE) {
+        constexpr int EACH = 16 / sizeof(A);
+#pragma unroll
+        for (int e = 0; e < MX_BLOCK; ++e)
+          ra[0][i].v[e / EACH][e % EACH] = e < left ? row[i][static_cast<int64_t>(whole) * MX_UNIT_K + e] : static_cast<A>(0.f);
+      }
+    }
+    multiply(0, true);
   }
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int64_t row = row_w + mx_row(i, lane & 15), col = col_w + (lane >> 4) * 8;
-    if (row >= p.m || col >= p.n) continue;
-    E* const c = static_cast<E*>(p.c) + row * p.ldc + col;
-    f32x8 v, old;
-    if constexpr (BETA) old = load_old(c, p.n - col);
+  for (int i = 0; i < UM; ++i)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      v[e] = p.alpha * acc[i][e >> 2][e & 3];
-      if constexpr (BETA) v[e] = __builtin_fmaf(p.beta, old[e], v[e]);
+    for (int q = 0; q < UN; ++q) sums[wave][i * UN + q][lane] = acc[i][q];
+  __syncthreads();
+  // four columns of a row per thread
+  for (int e = threadIdx.x; e < UM * UN * 64; e += 64 * WAVES) {
+    const int tile = e >> 6, l = e & 63;
+    f32x4 s = sums[0][tile][l];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) s += sums[w][tile][l];
+    const int64_t r = tile / UN * 16 + (l & 15), col = mx_row(part * UN + tile % UN, static_cast<int64_t>(l >> 4) * 4);
+    if (r >= m || col >= n) continue;
+    const float alpha = ps->pr[j].alpha, beta = ps->pr[j].beta;
+    const int64_t left = n - col, at = r * ps->pr[j].ldc + col;
+    auto finish = [&](auto* c) CANZ_INLINE {
+      using E = std::remove_pointer_t<decltype(c)>;
+      typedef E vec __attribute__((ext_vector_type(4), aligned(sizeof(E))));
+      float v[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        v[q] = alpha * s[q];
+        if (beta != 0.f && q < left) v[q] = __builtin_fmaf(beta, static_cast<float>(c[q]), v[q]);
+      }
+      if (left >= 4) {
+        *reinterpret_cast<vec*>(c) = vec{static_cast<E>(v[0]), static_cast<E>(v[1]), static_cast<E>(v[2]), static_cast<E>(v[3])};
+      } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (q < left) c[q] = static_cast<E>(v[q]);
+      }
+    };
+    void* const c = ps->pr[j].c;
+    if (ps->pr[j].out_dtype == CANZ_DT_F32)
+      finish(static_cast<float*>(c) + at);
+    else
+      finish(static_cast<__bf16*>(c) + at);
+  }
+}
+
+// ---- nothing along k: C <- beta C ---------------------------------------------------------------------------------------------
+__global__ __launch_bounds__(THREADS) void k_mx_scale(MxProblem p) {
+  const int64_t total = p.m * p.n;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * THREADS + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * THREADS) {
+    const int64_t at = i / p.n * p.ldc + i % p.n;
+    if (p.out_dtype == CANZ_DT_F32) {
+      float* const c = static_cast<float*>(p.c) + at;
+      *c = p.beta != 0.f ? p.beta * *c : 0.f;
+    } else {
+      __bf16* const c = static_cast<__bf16*>(p.c) + at;
+      *c = static_cast<__bf16>(p.beta != 0.f ? p.beta * static_cast<float>(*c) : 0.f);
     }
-    store_eight(c, p.n - col, v);
   }
 }
 
@@ -135,7 +339,6 @@ __global__ __launch_bounds__(THREADS) void k_mx_product_few(MxProblems ps) {
 // Four stages form a ring over the k units of all tiles of the block, one tile after another without a gap: while unit t is multiplied from
 // registers, the operands of t + 1 are read from LDS into a second set, t + 2 and t + 3 are in flight and t + 4 is requested into the stage of
 // t, which every wavefront has read before the barrier at the start of the step.  So there is one barrier per k unit, W W MFMAs long.
-constexpr int N_XCD = 8;
 constexpr int BAND = 4;   // tile rows that are walked column by column
 
 template <int W>
@@ -147,8 +350,6 @@ struct Stage {
 };
 
 // What a block has to do and has to load next: the tiles slot, slot + grid, ...
-// The kernel's argument where it lies: scalar loads at any index, and no copy of it.
-typedef const __attribute__((address_space(4))) MxProblems* KernArgs;
 struct Tile {
   int problem;   // -1: none
   int m0, n0;    // in units of 16 rows
@@ -179,12 +380,7 @@ __global__ __launch_bounds__(THREADS, W == 8 ? 1 : 2) void k_mx_product(MxProble
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1;
 
-  // the blocks of one XCD (blockIdx % 8) are neighbours in every round, a patch of tiles that share operands in its L2
-  int slot;
-  {
-    const int per = gridDim.x / N_XCD, rem = gridDim.x % N_XCD, xcd = blockIdx.x % N_XCD, q = blockIdx.x / N_XCD;
-    slot = xcd < rem ? xcd * (per + 1) + q : rem * (per + 1) + (xcd - rem) * per + q;
-  }
+  const int slot = xcd_slot();   // in every round the blocks of an XCD have a patch of tiles
 
   // ---- loading: this wavefront's pieces of the next four stages.  Every tile takes whole rounds of the ring, so its loop has no exit
   // inside and the accumulators stay where they are; units behind the last one are read from a page of zeros.
@@ -331,12 +527,12 @@ __global__ __launch_bounds__(THREADS, W == 8 ? 1 : 2) void k_mx_product(MxProble
   __builtin_amdgcn_s_waitcnt(wait_code(0));   // the requests behind the last tile have landed before the block leaves
 }
 
-// sets first_tile of every problem for square tiles of `edge`; the number of tiles
-int64_t count_tiles(MxProblems& ps, int edge) {
+// sets first_tile of every problem for tiles of rows x cols; the number of tiles
+int64_t count_tiles(MxProblems& ps, int rows, int cols) {
   int64_t tiles = 0;
   for (int i = 0; i < ps.n; ++i) {
     ps.pr[i].first_tile = static_cast<int>(tiles);
-    tiles += (ps.pr[i].m + edge - 1) / edge * ((ps.pr[i].n + edge - 1) / edge);
+    tiles += (ps.pr[i].m + rows - 1) / rows * ((ps.pr[i].n + cols - 1) / cols);
   }
   ps.tiles = static_cast<int>(tiles);
   return tiles;
@@ -345,45 +541,91 @@ int64_t count_tiles(MxProblems& ps, int edge) {
 constexpr int N_CU = 256;
 
 template <typename E, bool BETA>
-hipError_t launch_of(MxProblems& ps, hipStream_t st) {
-  // products of few rows (and of none along k) go to the kernel without LDS
-  MxProblems few, many;
-  few.n = many.n = 0;
-  for (int i = 0; i < ps.n; ++i) {
-    MxProblems& to = ps.pr[i].k == 0 || ps.pr[i].m <= FEW ? few : many;
-    to.pr[to.n++] = ps.pr[i];
-  }
-  if (few.n > 0) {
-    const int64_t tiles = count_tiles(few, FEW);
-    k_mx_product_few<E, BETA><<<dim3(static_cast<unsigned>(tiles)), THREADS, 0, st>>>(few);
-  }
-  if (many.n > 0) {
-    const int64_t tiles = count_tiles(many, 256);
-    if (tiles >= N_CU / 2) {
-      k_mx_product<8, E, BETA><<<dim3(static_cast<unsigned>(std::min<int64_t>(tiles, N_CU))), THREADS, 0, st>>>(many);
-    } else {
-      const int64_t small = count_tiles(many, 128);
-      k_mx_product<4, E, BETA><<<dim3(static_cast<unsigned>(std::min<int64_t>(small, 2 * N_CU))), THREADS, 0, st>>>(many);
-    }
+hipError_t launch_tiles(MxProblems& ps, hipStream_t st) {
+  const int64_t tiles = count_tiles(ps, 256, 256);
+  if (tiles >= N_CU / 2) {
+    k_mx_product<8, E, BETA><<<dim3(static_cast<unsigned>(std::min<int64_t>(tiles, N_CU))), THREADS, 0, st>>>(ps);
+  } else {
+    const int64_t small = count_tiles(ps, 128, 128);
+    k_mx_product<4, E, BETA><<<dim3(static_cast<unsigned>(std::min<int64_t>(small, 2 * N_CU))), THREADS, 0, st>>>(ps);
   }
   return hipGetLastError();
+}
+
+template <typename A, int UM, int UN, int WAVES, int AHEAD>
+hipError_t launch_few_as(MxProblems& ps, hipStream_t st) {
+  const int64_t blocks = count_tiles(ps, FEW_ROWS, UN * MX_UNIT_ROWS);
+  k_mx_product_few<A, UM, UN, WAVES, AHEAD><<<dim3(static_cast<unsigned>(blocks)), 64 * WAVES, 0, st>>>(ps);
+  return hipGetLastError();
+}
+
+// How the kernel for few rows goes over B, by its rows (a product alone decides, so that its sums do not depend on what shares the launch):
+// many of them are taken 64 to a block of four wavefronts, which halves what is read and rounded of A; with fewer the blocks are made smaller to fill the chip, and
+// with very few a block takes more wavefronts, so that k is gone through faster.  us for one row of bf16, 64 rows / 32 rows / 32 rows with 16 wavefronts:
+// 25600 x 5120 16.4 / 18.5 / 21.4, 12288 x 4096 6.9 / 7.5 / 8.2, 8192 x 5120 6.8 / 6.4 / 6.5, 5120 x 25600 24.1 / 19.2 / 20.1, 333 x 9000 9.2 / 8.0 / 6.8.
+enum Width { NARROW, MIDDLE, WIDE, WIDTHS };
+Width width_of(int64_t n) { return n >= 12288 ? WIDE : n >= 4096 ? MIDDLE : NARROW; }
+
+template <typename A, int UM, int AHEAD>
+hipError_t launch_few(MxProblems& ps, Width width, hipStream_t st) {
+  constexpr int MID = UM == 1 ? 4 : 8, SHORT = UM < 4 ? 16 : 8;   // wavefronts
+  constexpr int LESS = AHEAD < 2 ? AHEAD : 2;                     // 16 wavefronts have little of k each
+  switch (width) {
+    case NARROW: return launch_few_as<A, UM, 2, SHORT, LESS>(ps, st);
+    case MIDDLE: return launch_few_as<A, UM, 2, MID, AHEAD>(ps, st);
+    default: return launch_few_as<A, UM, 4, 4, AHEAD>(ps, st);
+  }
+}
+
+// The launches that a product may be part of.
+enum Kind { SCALE, TILES, IMAGE_16 = TILES + 4, IMAGE_32 = IMAGE_16 + WIDTHS, IMAGE_64 = IMAGE_32 + WIDTHS, ROUND_BF16 = IMAGE_64 + WIDTHS,
+            ROUND_F32 = ROUND_BF16 + WIDTHS, KINDS = ROUND_F32 + WIDTHS };
+int kind_of(const MxProblem& p) {
+  if (p.k == 0) return SCALE;
+  const Width w = width_of(p.n);
+  if (p.a_dtype != CANZ_DT_MX) return (p.a_dtype == CANZ_DT_BF16 ? ROUND_BF16 : ROUND_F32) + w;
+  if (p.m <= FEW_ROWS) return (p.m <= 16 ? IMAGE_16 : p.m <= 32 ? IMAGE_32 : IMAGE_64) + w;
+  return TILES + (p.out_dtype == CANZ_DT_F32 ? 0 : 1) + (p.beta != 0.f ? 2 : 0);
+}
+
+hipError_t launch_kind(int kind, MxProblems& ps, hipStream_t st) {
+  hipError_t err = hipSuccess;
+  switch (kind) {
+    case SCALE:
+      for (int i = 0; i < ps.n && err == hipSuccess; ++i) {
+        k_mx_scale<<<dim3(4 * N_CU), THREADS, 0, st>>>(ps.pr[i]);
+        err = hipGetLastError();
+      }
+      return err;
+    case TILES: return launch_tiles<float, false>(ps, st);
+    case TILES + 1: return launch_tiles<__bf16, false>(ps, st);
+    case TILES + 2: return launch_tiles<float, true>(ps, st);
+    case TILES + 3: return launch_tiles<__bf16, true>(ps, st);
+    default: break;
+  }
+  const Width w = static_cast<Width>((kind - IMAGE_16) % WIDTHS);
+  switch (kind - w) {
+    case IMAGE_16: return launch_few<uint8_t, 1, 4>(ps, w, st);
+    case IMAGE_32: return launch_few<uint8_t, 2, 3>(ps, w, st);
+    case IMAGE_64: return launch_few<uint8_t, 4, 2>(ps, w, st);
+    case ROUND_BF16: return launch_few<__bf16, 1, 4>(ps, w, st);
+    default: return launch_few<float, 1, 2>(ps, w, st);
+  }
 }
 
 }  // namespace
 
 hipError_t launch_mx_product(const MxProblems& ps, hipStream_t st) {
-  // a launch has one type of result, and reads the old one or not
-  for (int kind = 0; kind < 4; ++kind) {
+  int kind[MX_MAX_PROBLEMS];
+  for (int i = 0; i < ps.n; ++i) kind[i] = kind_of(ps.pr[i]);
+  for (int i = 0; i < ps.n; ++i) {
+    if (kind[i] < 0) continue;
     MxProblems part;
     part.n = 0;
-    for (int i = 0; i < ps.n; ++i)
-      if ((ps.pr[i].out_dtype == CANZ_DT_F32 ? 0 : 1) + (ps.pr[i].beta != 0.f ? 2 : 0) == kind) part.pr[part.n++] = ps.pr[i];
-    if (part.n == 0) continue;
-    const hipError_t err = kind == 0   ? launch_of<float, false>(part, st)
-                           : kind == 1 ? launch_of<__bf16, false>(part, st)
-                           : kind == 2 ? launch_of<float, true>(part, st)
-                                       : launch_of<__bf16, true>(part, st);
-    if (err != hipSuccess) return err;
+    const int now = kind[i];
+    for (int q = i; q < ps.n; ++q)
+      if (kind[q] == now) part.pr[part.n++] = ps.pr[q], kind[q] = -1;
+    if (const hipError_t err = launch_kind(now, part, st); err != hipSuccess) return err;
   }
   return hipSuccess;
 }

@@ -88,11 +88,14 @@ int check_product_group(const canz_mx_product_group& g, int idx, bool need_ptrs)
   return CANZ_OK;
 }
 
-// room for the image of every A that the call rounds itself
+// whether A is rounded by a launch of its own, into an image in the workspace
+bool mx_rounded_before(const canz_mx_product_group& g) { return !mx_idle(g) && g.k > 0 && g.a_dtype != CANZ_DT_MX && !mx_rounds_on_the_way(g.m, g.n, g.k); }
+
+// room for these images
 size_t product_workspace(const canz_mx_product_group* g, int32_t n_groups) {
   size_t need = 0;
   for (int i = 0; i < n_groups; ++i)
-    if (!mx_idle(g[i]) && g[i].a_dtype != CANZ_DT_MX) need += static_cast<size_t>(g[i].n_prods) * mx_image_bytes(g[i].m, g[i].k);
+    if (mx_rounded_before(g[i])) need += static_cast<size_t>(g[i].n_prods) * mx_image_bytes(g[i].m, g[i].k);
   return std::max(need, ALIGN);
 }
 
@@ -183,7 +186,8 @@ extern "C" int canz_mx_product(const canz_mx_product_group* g, int32_t n_groups,
     if (mx_idle(gi)) continue;
     uint8_t* const images = ws;
     const size_t each = static_cast<size_t>(mx_image_bytes(gi.m, gi.k));
-    if (gi.a_dtype != CANZ_DT_MX && gi.k > 0) {
+    const bool before = mx_rounded_before(gi);
+    if (before) {
       for (int first = 0; first < gi.n_prods; first += MX_MAX_MATS) {
         MxMats m{};
         m.rows = gi.m, m.cols = gi.k, m.ld = gi.lda;
@@ -200,7 +204,8 @@ extern "C" int canz_mx_product(const canz_mx_product_group* g, int32_t n_groups,
     }
     for (int x = 0; x < gi.n_prods; ++x) {
       MxProblem& p = ps.pr[ps.n++];
-      p.a = gi.a_dtype == CANZ_DT_MX ? static_cast<const uint8_t*>(gi.k > 0 ? gi.a[x] : nullptr) : images + x * each;
+      p.a = before ? images + x * each : static_cast<const uint8_t*>(gi.k > 0 ? gi.a[x] : nullptr);
+      p.a_dtype = before ? CANZ_DT_MX : gi.a_dtype, p.a_ceil = gi.a_scale_mode == CANZ_MX_SCALE_CEIL, p.lda = gi.lda;
       p.b = static_cast<const uint8_t*>(gi.k > 0 ? gi.b[x] : nullptr);
       p.c = gi.c[x];
       p.m = gi.m, p.n = gi.n, p.k = gi.k, p.ldc = gi.ldc;
