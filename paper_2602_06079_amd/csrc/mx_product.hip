@@ -36,6 +36,19 @@ __device__ __forceinline__ void static_for(F&& f) {
   static_for(f, std::make_integer_sequence<int, N>{});
 }
 
+// SIZE bytes a lane from base + lane_off + off straight into LDS, lane after lane; zeros beyond the `room` bytes of the buffer.
+template <int SIZE>
+__device__ __forceinline__ void buffer_to_lds(const uint8_t* base, unsigned room, __attribute__((address_space(3))) void* lds, int lane_off, int off) {
+#if defined(__HIP_DEVICE_COMPILE__)   // the descriptor's type is the device's only
+  constexpr int RAW = 0x00027000;     // a raw buffer of dwords
+  const auto buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), static_cast<short>(0), static_cast<int>(room), RAW);
+  if constexpr (SIZE == 16)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer, lds, 16, lane_off, off, 0, 0);
+  else
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer, lds, 4, lane_off, off, 0, 0);
+#endif
+}
+
 // Which of the launch's pieces of work this block has: the blocks of one XCD (blockIdx % 8) are neighbours, and share what they read in its L2.
 constexpr int N_XCD = 8;
 __device__ __forceinline__ int xcd_slot() {
@@ -366,8 +379,6 @@ __device__ __forceinline__ Tile tile_at(KernArgs ps, int logical) {
   return Tile{j, (band * BAND + in_band - tn * rows) * 2 * W, tn * 2 * W};
 }
 
-__device__ __attribute__((aligned(1024))) const uint8_t zero_page[MX_UNIT_BYTES] = {};
-
 template <int W, typename E, bool BETA>
 __global__ __launch_bounds__(THREADS, W == 8 ? 1 : 2) void k_mx_product(MxProblems) {
   using S = Stage<W>;
@@ -383,9 +394,13 @@ __global__ __launch_bounds__(THREADS, W == 8 ? 1 : 2) void k_mx_product(MxProble
   const int slot = xcd_slot();   // in every round the blocks of an XCD have a patch of tiles
 
   // ---- loading: this wavefront's pieces of the next four stages.  Every tile takes whole rounds of the ring, so its loop has no exit
-  // inside and the accumulators stay where they are; units behind the last one are read from a page of zeros.
+  // inside and the accumulators stay where they are; units behind the last one are asked for in an empty buffer, which gives zeros.
+  // Through buffer descriptors (of the tile's codes and scales of either operand) a load is one instruction beside its LDS address: the piece is the
+  // lane's offset, the unit a scalar one.
   int next_logical = slot, load_u = 0, load_ks = 0;
-  const uint8_t* src[S::loads];
+  const uint8_t *code_base[2], *scale_base[2];   // of A and B, from the tile's first unit on
+  unsigned code_room[2], scale_room[2];          // bytes there
+  int code_off[W], scale_off[S::scale_loads];    // this lane's part of its pieces
   auto next_round = [&]() CANZ_INLINE {
     load_u += 4;
     if (load_u < load_ks) return;
@@ -394,31 +409,41 @@ __global__ __launch_bounds__(THREADS, W == 8 ? 1 : 2) void k_mx_product(MxProble
     load_ks = 0;
     if (t.problem < 0) return;   // nothing left: zeros
     next_logical += gridDim.x;
-    const uint8_t *const a = ps->pr[t.problem].a, *const b = ps->pr[t.problem].b;
     load_ks = static_cast<int>(mx_k_units(ps->pr[t.problem].k));
-    const int units_m = static_cast<int>(mx_row_tiles(ps->pr[t.problem].m)), units_n = static_cast<int>(mx_row_tiles(ps->pr[t.problem].n));
-    const int64_t row_bytes = static_cast<int64_t>(load_ks) * MX_UNIT_BYTES, scale_bytes = static_cast<int64_t>(load_ks) * MX_SCALE_BYTES;
+    const int row_bytes = load_ks * MX_UNIT_BYTES, scale_bytes = load_ks * MX_SCALE_BYTES;   // 2^25 at most
+    int there[2];   // units of the tile that the image has
 #pragma unroll
-    for (int i = 0; i < W; ++i) {
-      const int piece = wave + 4 * i;   // of 4 W: A's, then B's
-      src[i] = piece < 2 * W ? a + min(t.m0 + piece, units_m - 1) * row_bytes : b + min(t.n0 + piece - 2 * W, units_n - 1) * row_bytes;
+    for (int o = 0; o < 2; ++o) {
+      const uint8_t* const image = o == 0 ? ps->pr[t.problem].a : ps->pr[t.problem].b;
+      const int units = static_cast<int>(mx_row_tiles(o == 0 ? ps->pr[t.problem].m : ps->pr[t.problem].n)), first = o == 0 ? t.m0 : t.n0;
+      there[o] = min(units - first, 2 * W);
+      code_base[o] = image + static_cast<int64_t>(first) * row_bytes, code_room[o] = static_cast<unsigned>(there[o]) * row_bytes;
+      scale_base[o] = image + static_cast<int64_t>(units) * row_bytes + static_cast<int64_t>(first / 4) * scale_bytes;
+      scale_room[o] = static_cast<unsigned>(there[o] / 4) * scale_bytes;
+    }
+#pragma unroll
+    for (int i = 0; i < W; ++i) {   // A's 2 W pieces, then B's; a unit that is not there is read as the last
+      const int o = i < W / 2 ? 0 : 1, piece = wave + 4 * i - o * 2 * W;
+      code_off[i] = min(piece, there[o] - 1) * row_bytes + lane * 16;
     }
 #pragma unroll
     for (int i = 0; i < S::scale_loads; ++i) {
-      const int piece = wave + 4 * i;   // of W
-      src[W + i] = piece < W / 2 ? a + units_m * row_bytes + min(t.m0 / 4 + piece, units_m / 4 - 1) * scale_bytes
-                                 : b + units_n * row_bytes + min(t.n0 / 4 + piece - W / 2, units_n / 4 - 1) * scale_bytes;
+      const int piece = wave + 4 * i, o = piece < W / 2 ? 0 : 1;
+      scale_off[i] = min(piece - o * (W / 2), there[o] / 4 - 1) * scale_bytes + lane * 4;
     }
   };
   auto fetch_one = [&](uint8_t* st, int u, auto idx) CANZ_INLINE {
     constexpr int I = decltype(idx)::value;
     const bool there = u < load_ks;
     if constexpr (I < W) {
-      const uint8_t* const from = there ? src[I] + static_cast<int64_t>(u) * MX_UNIT_BYTES : zero_page;
-      __builtin_amdgcn_global_load_lds(CANZ_GLB(from + lane * 16), CANZ_LDS(st + (wave + 4 * I) * MX_UNIT_BYTES), 16, 0, 0);
+      constexpr int o = I < W / 2 ? 0 : 1;
+      buffer_to_lds<16>(code_base[o], there ? code_room[o] : 0u, CANZ_LDS(st + (wave + 4 * I) * MX_UNIT_BYTES), code_off[I],
+                        there ? u * MX_UNIT_BYTES : 0);
     } else {
-      const uint8_t* const from = there ? src[I] + static_cast<int64_t>(u) * MX_SCALE_BYTES : zero_page;
-      __builtin_amdgcn_global_load_lds(CANZ_GLB(from + lane * 4), CANZ_LDS(st + 2 * S::codes + (wave + 4 * (I - W)) * MX_SCALE_BYTES), 4, 0, 0);
+      constexpr int i = I - W;
+      const int o = S::scale_loads == 2 ? i : wave < W / 2 ? 0 : 1;
+      buffer_to_lds<4>(o == 0 ? scale_base[0] : scale_base[1], there ? (o == 0 ? scale_room[0] : scale_room[1]) : 0u,
+                       CANZ_LDS(st + 2 * S::codes + (wave + 4 * i) * MX_SCALE_BYTES), scale_off[i], there ? u * MX_SCALE_BYTES : 0);
     }
   };
 
