@@ -82,19 +82,24 @@ __device__ __forceinline__ f32x8 load_old(const E* c, int64_t left) {
   }
   return v;
 }
+// 16 bytes of a row of C, of which `left` elements are there.
 template <typename E>
-__device__ __forceinline__ void store_eight(E* c, int64_t left, f32x8 v) {
-  if (left >= 8) {
-    typedef E vec __attribute__((ext_vector_type(8), aligned(sizeof(E))));
-    vec x;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = static_cast<E>(v[e]);
-    *reinterpret_cast<vec*>(c) = x;
+__device__ __forceinline__ void store_piece(E* c, int64_t left, i32x4 v) {
+  constexpr int N = 16 / sizeof(E);
+  if (left >= N) {
+    typedef E any __attribute__((ext_vector_type(N), aligned(sizeof(E))));
+    *reinterpret_cast<any*>(c) = __builtin_bit_cast(any, v);
   } else {
 #pragma unroll 1
-    for (int e = 0; e < left; ++e) {
-      c[e] = static_cast<E>(v[0]);
-      v = f32x8{v[1], v[2], v[3], v[4], v[5], v[6], v[7], 0.f};
+    for (int e = 0; e < left; ++e) {   // a rolled loop: the piece moves down instead of being indexed
+      if constexpr (sizeof(E) == 4) {
+        c[e] = __builtin_bit_cast(float, v[0]);
+        v = i32x4{v[1], v[2], v[3], 0};
+      } else {
+        c[e] = __builtin_bit_cast(__bf16, static_cast<short>(v[0]));
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = static_cast<int>(static_cast<unsigned>(v[q]) >> 16 | (q < 3 ? static_cast<unsigned>(v[q < 3 ? q + 1 : 3]) << 16 : 0u));
+      }
     }
   }
 }
@@ -497,25 +502,55 @@ __global__ __launch_bounds__(THREADS, W == 8 ? 1 : 2) void k_mx_product(MxProble
     const int64_t row0 = (t.m0 + wm * W) * MX_UNIT_ROWS, col0 = (t.n0 + wn * W) * MX_UNIT_ROWS + (lane >> 4) * 8;
     const int64_t left = ps->pr[t.problem].n - col0;   // columns from this lane's first one on
     const float alpha = ps->pr[t.problem].alpha, beta = ps->pr[t.problem].beta;
-    E* const c = static_cast<E*>(ps->pr[t.problem].c) + col0;
+    E* const c = static_cast<E*>(ps->pr[t.problem].c);
+    // Pieces of 16 bytes leave in pairs (the two halves of eight fp32 results, or two neighbouring pairs of units in bf16), which lanes 8 apart
+    // exchange, so that a store instruction has 8 rows of 128 bytes instead of 16 of 64 or of every other 16.
+    constexpr int APART = sizeof(E) == 4 ? 4 : 32;   // columns from one of a pair to the other
+    constexpr int PAIRS = sizeof(E) == 4 ? W / 2 : W / 4, STEP = sizeof(E) == 4 ? 32 : 64;
+    const int slot = lane & 15, out_col = slot < 8 ? 0 : APART;
 #pragma unroll
     for (int i = 0; i < W; ++i) {
-      const int64_t row = row0 + mx_row(i, lane & 15);
-      if (row < rows) {
-        E* const at = c + row * ldc;
+      float v[W / 2][8];   // this lane's row, eight columns of every pair of units
+#pragma unroll
+      for (int e = 0; e < W * 4; ++e) v[e >> 3][e & 7] = alpha * acc[i][e >> 2][e & 3];
+      if constexpr (BETA) {
+        const int64_t row = row0 + mx_row(i, slot);
         f32x8 old[W / 2];
-        if constexpr (BETA)
+        if (row < rows) {
 #pragma unroll
-          for (int jp = 0; jp < W / 2; ++jp) old[jp] = load_old(at + jp * 32, left - jp * 32);
+          for (int jp = 0; jp < W / 2; ++jp) old[jp] = load_old(c + row * ldc + col0 + jp * 32, left - jp * 32);
 #pragma unroll
-        for (int jp = 0; jp < W / 2; ++jp) {
-          f32x8 v;
+          for (int e = 0; e < W * 4; ++e) v[e >> 3][e & 7] = __builtin_fmaf(beta, old[e >> 3][e & 7], v[e >> 3][e & 7]);
+        }
+      }
+      i32x4 low[PAIRS], high[PAIRS];   // rows of slots 0 .. 7 and 8 .. 15
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            v[e] = alpha * acc[i][2 * jp + (e >> 2)][e & 3];
-            if constexpr (BETA) v[e] = __builtin_fmaf(beta, old[jp][e], v[e]);
+      for (int q = 0; q < PAIRS; ++q) {
+        i32x4 x, y;
+        if constexpr (sizeof(E) == 4) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = __builtin_bit_cast(int, v[q][e]), y[e] = __builtin_bit_cast(int, v[q][4 + e]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            x[e] = __builtin_bit_cast(int, mx_bf16x2{static_cast<__bf16>(v[2 * q][2 * e]), static_cast<__bf16>(v[2 * q][2 * e + 1])});
+            y[e] = __builtin_bit_cast(int, mx_bf16x2{static_cast<__bf16>(v[2 * q + 1][2 * e]), static_cast<__bf16>(v[2 * q + 1][2 * e + 1])});
           }
-          store_eight(at + jp * 32, left - jp * 32, v);
+        }
+        constexpr int ROTATE_8 = 0x128;   // within 16 lanes; the bank masks are their last and first eight
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          low[q][e] = __builtin_amdgcn_update_dpp(x[e], y[e], ROTATE_8, 0xF, 0xC, false);
+          high[q][e] = __builtin_amdgcn_update_dpp(y[e], x[e], ROTATE_8, 0xF, 0x3, false);
+        }
+      }
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int64_t row = row0 + mx_row(i, half * 8 + (slot & 7));
+        if (row < rows) {
+          E* const at = c + row * ldc + col0 + out_col;
+#pragma unroll
+          for (int q = 0; q < PAIRS; ++q) store_piece(at + q * STEP, left - out_col - q * STEP, half == 0 ? low[q] : high[q]);
         }
       }
       CANZ_FENCE();
