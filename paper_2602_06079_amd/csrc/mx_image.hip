@@ -18,13 +18,18 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 // Code of one element with noise u in 0 .. 255: s floor((rint(256 a / s) + u) / 256) for a = |v| / X and the distance s of the values
-// around it.  Every step before the rint is exact, and it and the sum are integers below 2^11.
+// around it, s = 2^(e - 1) with e the exponent of a, at least 0.  Adding 1.5 2^23 (s / 256) rounds a to a multiple of s / 256, ties to even, and leaves
+// that multiple in the low bits of the sum; with 2 e s added as well, bits 8 and up are the code after u is added to them.  The largest sums are those of e
+// = 2, so that one limit keeps the code at 7.
 __device__ __forceinline__ unsigned noisy_code(float v, unsigned byte, unsigned u) {
   const float a = __builtin_amdgcn_ldexpf(__builtin_fabsf(v), 127 - static_cast<int>(byte));
-  const int shift = a < 2.f ? 9 : a < 4.f ? 8 : 7;
-  const unsigned n = (static_cast<unsigned>(__builtin_rintf(__builtin_amdgcn_ldexpf(a, shift))) + u) >> 8;
-  const unsigned code = min(n + (a < 2.f ? 0u : a < 4.f ? 2u : 4u), 7u);
-  return code | (__builtin_bit_cast(unsigned, v) >> 31 << 3);
+  const unsigned e = max(__builtin_bit_cast(unsigned, a) >> 23, 127u);   // + 127
+  // bits of 1.5 2^(e + 14) + 2 e s: (e + 127 + 14) << 23 | 1 << 22 | e << 9
+  constexpr unsigned STEP = (1u << 23) + (1u << 9), START = (14u << 23) + (1u << 22) - (127u << 9);
+  constexpr unsigned LIMIT = ((2u + 127u + 14u) << 23) + (1u << 22) + 0x7FFu;
+  const float magic = __builtin_bit_cast(float, __umul24(e, STEP) + START);
+  const unsigned sum = min(__builtin_bit_cast(unsigned, a + magic) + u, LIMIT);
+  return (sum >> 8 & 7u) | (__builtin_bit_cast(unsigned, v) >> 31 << 3);
 }
 // eight codes of one block, element 0 in the lowest bits
 template <bool NOISE>
@@ -137,31 +142,40 @@ __global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {
   }
   __syncthreads();
   if constexpr (COL) {
-    const int c = t & (TILE - 1);
+    // two neighbouring columns of 32 rows per thread: one LDS access takes both
+    typedef E pair __attribute__((ext_vector_type(2)));
+    const int c = (t & 63) * 2, rb = t >> 6;
     const int64_t unit = mx_unit(c0 + c);
+    float v[2][MX_BLOCK];
+    unsigned long long u[2][4] = {};
+    unsigned amax[2] = {0, 0};
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int rb = (t >> 7) + 2 * i;
-      unsigned amax = 0;
+    for (int e = 0; e < MX_BLOCK; ++e) {
+      const int at = (rb * MX_BLOCK + e) * TILE + c;
+      const pair x = *reinterpret_cast<const pair*>(tile + at);
+      unsigned n = 0;
+      if constexpr (NOISE) n = *reinterpret_cast<const unsigned short*>(tile_noise + at);
 #pragma unroll
-      for (int e = 0; e < MX_BLOCK; ++e) amax = max(amax, mx_magnitude(static_cast<float>(tile[(rb * MX_BLOCK + e) * TILE + c])));
-      const unsigned byte = mx_scale_byte(amax, ceil);
+      for (int q = 0; q < 2; ++q) {
+        v[q][e] = static_cast<float>(x[q]);
+        amax[q] = max(amax[q], mx_magnitude(v[q][e]));
+        if constexpr (NOISE) u[q][e >> 3] |= static_cast<unsigned long long>(n >> (8 * q) & 255u) << (8 * (e & 7));
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const unsigned byte = mx_scale_byte(amax[q], ceil);
       u32x4 codes;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        float v[8];
-        unsigned long long u = 0;
+      for (int w = 0; w < 4; ++w) {
+        float part[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int at = (rb * MX_BLOCK + q * 8 + e) * TILE + c;
-          v[e] = static_cast<float>(tile[at]);
-          if constexpr (NOISE) u |= static_cast<unsigned long long>(tile_noise[at]) << (8 * e);
-        }
-        codes[q] = eight_codes<NOISE>(v, byte, u);
+        for (int e = 0; e < 8; ++e) part[e] = v[q][w * 8 + e];
+        codes[w] = eight_codes<NOISE>(part, byte, u[q][w]);
       }
       if (unit < mx_row_tiles(m.cols))
-        *reinterpret_cast<u32x4*>(m.by_col[which] + (unit * units_col + r0 / MX_UNIT_K) * MX_UNIT_BYTES + (rb * 16 + mx_slot(c)) * 16) = codes;
-      reinterpret_cast<uint8_t*>(scales[1][c >> 6])[(rb * 16 + mx_slot(c)) * 4 + mx_unit(c) % 4] = static_cast<uint8_t>(byte);
+        *reinterpret_cast<u32x4*>(m.by_col[which] + (unit * units_col + r0 / MX_UNIT_K) * MX_UNIT_BYTES + (rb * 16 + mx_slot(c + q)) * 16) = codes;
+      reinterpret_cast<uint8_t*>(scales[1][c >> 6])[(rb * 16 + mx_slot(c + q)) * 4 + mx_unit(c) % 4] = static_cast<uint8_t>(byte);
     }
     __syncthreads();
   }

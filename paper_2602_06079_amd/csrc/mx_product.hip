@@ -600,13 +600,26 @@ int64_t count_tiles(MxProblems& ps, int rows, int cols) {
 
 constexpr int N_CU = 256;
 
+// ns that a launch takes by the tiles it has: 256 x 256 in rounds of one to a CU, 128 x 128 in rounds of two, or less than one at the end.  A k unit
+// takes 780 ns of a round of large tiles and 460 of one of small ones (a quarter of the work, twice as often), 210 with one small tile to a CU; beginning
+// and end of a tile 6000 and 2600.  us, 256 x 256 and 128 x 128: 8192^3 229, 256; 4096^3 36, 39; 8192 x 12288 x 4096 195, 212; 4096 x 25600 x 5120 269, 269;
+// 6000 x 6000 x 2000 61, 50; 4096 x 4096 x 1024 17.5, 16.4; 2048 x 4096 x 8192 51, 35; 4096 x 2048 x 1024 16.2, 10.8; 1024^3 13.3, 6.1.
+int64_t large_tiles_ns(int64_t tiles, int64_t ks) { return (tiles + N_CU - 1) / N_CU * (780 * ks + 6000); }
+int64_t small_tiles_ns(int64_t tiles, int64_t ks) {
+  const int64_t rest = tiles % (2 * N_CU);
+  return tiles / (2 * N_CU) * (460 * ks + 2600) + (rest > N_CU ? 460 * ks + 2600 : rest > 0 ? 210 * ks + 2600 : 0);
+}
+
 template <typename E, bool BETA>
 hipError_t launch_tiles(MxProblems& ps, hipStream_t st) {
-  const int64_t tiles = count_tiles(ps, 256, 256);
-  if (tiles >= N_CU / 2) {
-    k_mx_product<8, E, BETA><<<dim3(static_cast<unsigned>(std::min<int64_t>(tiles, N_CU))), THREADS, 0, st>>>(ps);
+  const int64_t large = count_tiles(ps, 256, 256), small = count_tiles(ps, 128, 128);
+  int64_t units = 0;   // of all small tiles along k
+  for (int i = 0; i < ps.n; ++i) units += ((i + 1 < ps.n ? ps.pr[i + 1].first_tile : small) - ps.pr[i].first_tile) * mx_k_units(ps.pr[i].k);
+  const int64_t ks = (units + small - 1) / small;
+  if (large_tiles_ns(large, ks) < small_tiles_ns(small, ks)) {
+    count_tiles(ps, 256, 256);
+    k_mx_product<8, E, BETA><<<dim3(static_cast<unsigned>(std::min<int64_t>(large, N_CU))), THREADS, 0, st>>>(ps);
   } else {
-    const int64_t small = count_tiles(ps, 128, 128);
     k_mx_product<4, E, BETA><<<dim3(static_cast<unsigned>(std::min<int64_t>(small, 2 * N_CU))), THREADS, 0, st>>>(ps);
   }
   return hipGetLastError();
