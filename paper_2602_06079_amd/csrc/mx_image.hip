@@ -31,14 +31,13 @@ __device__ __forceinline__ unsigned noisy_code(float v, unsigned byte, unsigned 
   const unsigned sum = min(__builtin_bit_cast(unsigned, a + magic) + u, LIMIT);
   return (sum >> 8 & 7u) | (__builtin_bit_cast(unsigned, v) >> 31 << 3);
 }
-// eight codes of one block, element 0 in the lowest bits
+// eight codes of one block, element 0 in the lowest bits; u: noise bytes
 template <bool NOISE>
-__device__ __forceinline__ unsigned eight_codes(const float (&v)[8], unsigned byte, unsigned long long noise) {
-  if (byte == MX_SCALE_NAN) return 0;
+__device__ __forceinline__ unsigned eight_codes(const float (&v)[8], unsigned byte, const unsigned (&u)[8]) {
   unsigned r = 0;
   if constexpr (NOISE) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) r |= noisy_code(v[i], byte, static_cast<unsigned>(noise >> (8 * i)) & 255u) << (4 * i);
+    for (int i = 0; i < 8; ++i) r |= noisy_code(v[i], byte, u[i]) << (4 * i);
   } else {
     const float s = mx_scale_value(byte);
     r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[0], v[1], s, 0);
@@ -46,7 +45,14 @@ __device__ __forceinline__ unsigned eight_codes(const float (&v)[8], unsigned by
     r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[4], v[5], s, 2);
     r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[6], v[7], s, 3);
   }
-  return r;
+  return byte == MX_SCALE_NAN ? 0u : r;
+}
+
+// the largest of the four lanes that hold a block
+__device__ __forceinline__ unsigned largest_of_four(unsigned v) {
+  constexpr int SWAP_1 = 0xB1, SWAP_2 = 0x4E;   // quad permutes [1, 0, 3, 2] and [2, 3, 0, 1]
+  v = max(v, static_cast<unsigned>(__builtin_amdgcn_mov_dpp(static_cast<int>(v), SWAP_1, 0xF, 0xF, false)));
+  return max(v, static_cast<unsigned>(__builtin_amdgcn_mov_dpp(static_cast<int>(v), SWAP_2, 0xF, 0xF, false)));
 }
 
 // eight consecutive elements of a row, those behind its end as zeros
@@ -67,11 +73,14 @@ __device__ __forceinline__ void load8(const E* p, int64_t left, float (&v)[8]) {
     for (int i = 0; i < 8; ++i) v[i] = i < left ? static_cast<float>(p[i]) : 0.f;
   }
 }
-__device__ __forceinline__ unsigned long long load_noise8(const uint8_t* p, int64_t left) {
-  if (left >= 8) return __builtin_bit_cast(unsigned long long, *reinterpret_cast<const u32x2_any*>(p));
-  unsigned long long r = 0;
+__device__ __forceinline__ uint2 load_noise8(const uint8_t* p, int64_t left) {
+  if (left >= 8) {
+    const u32x2_any w = *reinterpret_cast<const u32x2_any*>(p);
+    return uint2{w[0], w[1]};
+  }
+  uint2 r = {0, 0};
 #pragma unroll
-  for (int i = 0; i < 8; ++i) r |= i < left ? static_cast<unsigned long long>(p[i]) << (8 * i) : 0ull;
+  for (int i = 0; i < 8; ++i) (i < 4 ? r.x : r.y) |= i < left ? static_cast<unsigned>(p[i]) << (8 * (i & 3)) : 0u;
   return r;
 }
 template <typename E>
@@ -117,20 +126,21 @@ __global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {
     const int64_t left = r0 + row < m.rows ? m.cols - (c0 + col) : 0;
     float v[8];
     load8(src + (r0 + row) * m.ld + c0 + col, left, v);
-    unsigned long long u = 0;
-    if constexpr (NOISE) u = load_noise8(noise + (r0 + row) * m.cols + c0 + col, left);
+    uint2 noise8 = {0, 0};
+    if constexpr (NOISE) noise8 = load_noise8(noise + (r0 + row) * m.cols + c0 + col, left);
     if constexpr (COL) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) tile[row * TILE + col + e] = static_cast<E>(v[e]);
-      if constexpr (NOISE) *reinterpret_cast<unsigned long long*>(tile_noise + row * TILE + col) = u;
+      if constexpr (NOISE) *reinterpret_cast<uint2*>(tile_noise + row * TILE + col) = noise8;
     }
     if constexpr (ROW) {
       unsigned amax = 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) amax = max(amax, mx_magnitude(v[e]));
-      amax = max(amax, static_cast<unsigned>(__shfl_xor(static_cast<int>(amax), 1, 64)));
-      amax = max(amax, static_cast<unsigned>(__shfl_xor(static_cast<int>(amax), 2, 64)));
-      const unsigned byte = mx_scale_byte(amax, ceil);
+      const unsigned byte = mx_scale_byte(largest_of_four(amax), ceil);
+      unsigned u[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) u[e] = (e < 4 ? noise8.x : noise8.y) >> (8 * (e & 3)) & 255u;
       const unsigned codes = eight_codes<NOISE>(v, byte, u);
       const int kb = (t & 15) >> 2;
       const int64_t unit = mx_unit(r0 + row);
@@ -147,19 +157,18 @@ __global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {
     const int c = (t & 63) * 2, rb = t >> 6;
     const int64_t unit = mx_unit(c0 + c);
     float v[2][MX_BLOCK];
-    unsigned long long u[2][4] = {};
+    unsigned n[MX_BLOCK];   // the noise of both
     unsigned amax[2] = {0, 0};
 #pragma unroll
     for (int e = 0; e < MX_BLOCK; ++e) {
       const int at = (rb * MX_BLOCK + e) * TILE + c;
       const pair x = *reinterpret_cast<const pair*>(tile + at);
-      unsigned n = 0;
-      if constexpr (NOISE) n = *reinterpret_cast<const unsigned short*>(tile_noise + at);
+      n[e] = 0;
+      if constexpr (NOISE) n[e] = *reinterpret_cast<const unsigned short*>(tile_noise + at);
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
         v[q][e] = static_cast<float>(x[q]);
         amax[q] = max(amax[q], mx_magnitude(v[q][e]));
-        if constexpr (NOISE) u[q][e >> 3] |= static_cast<unsigned long long>(n >> (8 * q) & 255u) << (8 * (e & 7));
       }
     }
 #pragma unroll
@@ -169,9 +178,10 @@ __global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         float part[8];
+        unsigned u[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) part[e] = v[q][w * 8 + e];
-        codes[w] = eight_codes<NOISE>(part, byte, u[q][w]);
+        for (int e = 0; e < 8; ++e) part[e] = v[q][w * 8 + e], u[e] = n[w * 8 + e] >> (8 * q) & 255u;
+        codes[w] = eight_codes<NOISE>(part, byte, u);
       }
       if (unit < mx_row_tiles(m.cols))
         *reinterpret_cast<u32x4*>(m.by_col[which] + (unit * units_col + r0 / MX_UNIT_K) * MX_UNIT_BYTES + (rb * 16 + mx_slot(c + q)) * 16) = codes;
