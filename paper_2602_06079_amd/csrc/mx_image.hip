@@ -104,25 +104,26 @@ __device__ __forceinline__ void store8(E* p, int64_t left, const float (&v)[8]) 
   }
 }
 
-// One block rounds a tile of 128 x 128 elements: first along its rows (16 lanes a row, 8 elements each, 4 lanes a block), keeping
-// the elements in LDS, then along its columns (a thread a block).  Scale bytes are collected in LDS and leave as whole units.
+// One block rounds a tile of 128 rows x 64 columns: first along its rows (8 lanes a row, 8 elements each, 4 lanes a block), keeping
+// the elements in LDS, then along its columns (a thread two blocks).  Scale bytes are collected in LDS and leave in pieces of 128 bytes and more.
+constexpr int ROWS = 128, COLS = 64;
 template <typename E, bool ROW, bool COL, bool NOISE>
 __global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {
-  __shared__ E tile[COL ? TILE * TILE : 1];
-  __shared__ uint8_t tile_noise[COL && NOISE ? TILE * TILE : 1];
-  __shared__ unsigned scales[2][2][MX_SCALE_BYTES / 4];
-  const int t = threadIdx.x, which = blockIdx.y;
-  const int64_t tiles_c = (m.cols + TILE - 1) / TILE;
-  const int64_t r0 = blockIdx.x / tiles_c * TILE, c0 = blockIdx.x % tiles_c * TILE;
+  __shared__ E tile[COL ? ROWS * COLS : 1];
+  __shared__ uint8_t tile_noise[COL && NOISE ? ROWS * COLS : 1];
+  __shared__ unsigned row_scales[2][2][16], col_scales[4][16];   // 64 rows, block, slot; block, slot: dwords of the units' order
+  const int t = threadIdx.x, which = blockIdx.z;
+  const int64_t r0 = static_cast<int64_t>(blockIdx.y) * ROWS, c0 = static_cast<int64_t>(blockIdx.x) * COLS;
   const E* const src = static_cast<const E*>(m.mat[which]);
   const uint8_t* const noise = NOISE ? m.noise[which] : nullptr;
   const int ceil = m.scale_mode == CANZ_MX_SCALE_CEIL;
   const int64_t units_row = mx_k_units(m.cols), units_col = mx_k_units(m.rows);   // k units of the two images
+  const int kb0 = static_cast<int>(c0 / MX_BLOCK) & 3;                            // 0 or 2: the tile is one half of a k unit of by_row
 
-  const int col = (t & 15) * 8;
-#pragma unroll 4
-  for (int i = 0; i < TILE / 16; ++i) {
-    const int row = i * 16 + (t >> 4);
+  const int col = (t & 7) * 8;
+#pragma unroll
+  for (int i = 0; i < ROWS / 32; ++i) {
+    const int row = i * 32 + (t >> 3);
     const int64_t left = r0 + row < m.rows ? m.cols - (c0 + col) : 0;
     float v[8];
     load8(src + (r0 + row) * m.ld + c0 + col, left, v);
@@ -130,8 +131,8 @@ __global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {
     if constexpr (NOISE) noise8 = load_noise8(noise + (r0 + row) * m.cols + c0 + col, left);
     if constexpr (COL) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) tile[row * TILE + col + e] = static_cast<E>(v[e]);
-      if constexpr (NOISE) *reinterpret_cast<uint2*>(tile_noise + row * TILE + col) = noise8;
+      for (int e = 0; e < 8; ++e) tile[row * COLS + col + e] = static_cast<E>(v[e]);
+      if constexpr (NOISE) *reinterpret_cast<uint2*>(tile_noise + row * COLS + col) = noise8;
     }
     if constexpr (ROW) {
       unsigned amax = 0;
@@ -142,60 +143,61 @@ __global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) u[e] = (e < 4 ? noise8.x : noise8.y) >> (8 * (e & 3)) & 255u;
       const unsigned codes = eight_codes<NOISE>(v, byte, u);
-      const int kb = (t & 15) >> 2;
+      const int kb = (t & 7) >> 2;
       const int64_t unit = mx_unit(r0 + row);
       if (unit < mx_row_tiles(m.rows))
-        *reinterpret_cast<unsigned*>(m.by_row[which] + (unit * units_row + c0 / MX_UNIT_K) * MX_UNIT_BYTES + (kb * 16 + mx_slot(row)) * 16 +
+        *reinterpret_cast<unsigned*>(m.by_row[which] + (unit * units_row + c0 / MX_UNIT_K) * MX_UNIT_BYTES + ((kb0 + kb) * 16 + mx_slot(row)) * 16 +
                                      (t & 3) * 4) = codes;
-      if ((t & 3) == 0) reinterpret_cast<uint8_t*>(scales[0][row >> 6])[(kb * 16 + mx_slot(row)) * 4 + mx_unit(row) % 4] = static_cast<uint8_t>(byte);
+      if ((t & 3) == 0) reinterpret_cast<uint8_t*>(&row_scales[row >> 6][kb][mx_slot(row)])[mx_unit(row) % 4] = static_cast<uint8_t>(byte);
     }
   }
   __syncthreads();
   if constexpr (COL) {
     // two neighbouring columns of 32 rows per thread: one LDS access takes both
     typedef E pair __attribute__((ext_vector_type(2)));
-    const int c = (t & 63) * 2, rb = t >> 6;
-    const int64_t unit = mx_unit(c0 + c);
-    float v[2][MX_BLOCK];
-    unsigned n[MX_BLOCK];   // the noise of both
-    unsigned amax[2] = {0, 0};
+    const int c = (t & 31) * 2, rb = t >> 5;
+    if (rb < ROWS / MX_BLOCK && c0 < m.cols) {
+      float v[2][MX_BLOCK];
+      unsigned n[MX_BLOCK];   // the noise of both
+      unsigned amax[2] = {0, 0};
 #pragma unroll
-    for (int e = 0; e < MX_BLOCK; ++e) {
-      const int at = (rb * MX_BLOCK + e) * TILE + c;
-      const pair x = *reinterpret_cast<const pair*>(tile + at);
-      n[e] = 0;
-      if constexpr (NOISE) n[e] = *reinterpret_cast<const unsigned short*>(tile_noise + at);
+      for (int e = 0; e < MX_BLOCK; ++e) {
+        const int at = (rb * MX_BLOCK + e) * COLS + c;
+        const pair x = *reinterpret_cast<const pair*>(tile + at);
+        n[e] = 0;
+        if constexpr (NOISE) n[e] = *reinterpret_cast<const unsigned short*>(tile_noise + at);
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          v[q][e] = static_cast<float>(x[q]);
+          amax[q] = max(amax[q], mx_magnitude(v[q][e]));
+        }
+      }
+      const int64_t unit = mx_unit(c0 + c);
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
-        v[q][e] = static_cast<float>(x[q]);
-        amax[q] = max(amax[q], mx_magnitude(v[q][e]));
-      }
-    }
+        const unsigned byte = mx_scale_byte(amax[q], ceil);
+        u32x4 codes;
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const unsigned byte = mx_scale_byte(amax[q], ceil);
-      u32x4 codes;
+        for (int w = 0; w < 4; ++w) {
+          float part[8];
+          unsigned u[8];
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        float part[8];
-        unsigned u[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) part[e] = v[q][w * 8 + e], u[e] = n[w * 8 + e] >> (8 * q) & 255u;
-        codes[w] = eight_codes<NOISE>(part, byte, u);
-      }
-      if (unit < mx_row_tiles(m.cols))
+          for (int e = 0; e < 8; ++e) part[e] = v[q][w * 8 + e], u[e] = n[w * 8 + e] >> (8 * q) & 255u;
+          codes[w] = eight_codes<NOISE>(part, byte, u);
+        }
         *reinterpret_cast<u32x4*>(m.by_col[which] + (unit * units_col + r0 / MX_UNIT_K) * MX_UNIT_BYTES + (rb * 16 + mx_slot(c + q)) * 16) = codes;
-      reinterpret_cast<uint8_t*>(scales[1][c >> 6])[(rb * 16 + mx_slot(c + q)) * 4 + mx_unit(c) % 4] = static_cast<uint8_t>(byte);
+        reinterpret_cast<uint8_t*>(&col_scales[rb][mx_slot(c + q)])[mx_unit(c) % 4] = static_cast<uint8_t>(byte);
+      }
     }
     __syncthreads();
   }
-  const int half = (t >> 6) & 1, word = t & 63;
-  if (ROW && t < 128 && r0 + half * MX_PAD_ROWS < m.rows)
+  const int half = t >> 5 & 1, word = t & 31;
+  if (ROW && t < 64 && r0 + half * MX_PAD_ROWS < m.rows)
     *reinterpret_cast<unsigned*>(m.by_row[which] + mx_code_bytes(m.rows, m.cols) +
-                                 ((r0 / MX_PAD_ROWS + half) * units_row + c0 / MX_UNIT_K) * MX_SCALE_BYTES + word * 4) = scales[0][half][word];
-  if (COL && t >= 128 && c0 + half * MX_PAD_ROWS < m.cols)
+                                 ((r0 / MX_PAD_ROWS + half) * units_row + c0 / MX_UNIT_K) * MX_SCALE_BYTES + (kb0 * 16 + word) * 4) = row_scales[half][word >> 4][word & 15];
+  if (COL && t >= 64 && t < 128 && c0 < m.cols)
     *reinterpret_cast<unsigned*>(m.by_col[which] + mx_code_bytes(m.cols, m.rows) +
-                                 ((c0 / MX_PAD_ROWS + half) * units_col + r0 / MX_UNIT_K) * MX_SCALE_BYTES + word * 4) = scales[1][half][word];
+                                 (c0 / MX_PAD_ROWS * units_col + r0 / MX_UNIT_K) * MX_SCALE_BYTES + (t - 64) * 4) = col_scales[(t - 64) >> 4][t & 15];
 }
 
 __device__ __forceinline__ void eight_values(unsigned codes, unsigned byte, float (&v)[8]) {
@@ -213,9 +215,8 @@ template <typename E, bool COL>
 __global__ __launch_bounds__(THREADS) void k_mx_dequantize(MxMats m) {
   constexpr int LDT = TILE + 8 / sizeof(E);
   __shared__ E tile[COL ? TILE * LDT : 1];
-  const int t = threadIdx.x, which = blockIdx.y;
-  const int64_t tiles_c = (m.cols + TILE - 1) / TILE;
-  const int64_t r0 = blockIdx.x / tiles_c * TILE, c0 = blockIdx.x % tiles_c * TILE;
+  const int t = threadIdx.x, which = blockIdx.z;
+  const int64_t r0 = static_cast<int64_t>(blockIdx.y) * TILE, c0 = static_cast<int64_t>(blockIdx.x) * TILE;
   E* const dst = static_cast<E*>(m.mat[which]);
   if constexpr (COL) {
     const uint8_t* const img = m.by_col[which];
@@ -262,18 +263,23 @@ __global__ __launch_bounds__(THREADS) void k_mx_dequantize(MxMats m) {
   }
 }
 
-dim3 tiles_of(const MxMats& m) {
-  return dim3(static_cast<unsigned>((m.rows + TILE - 1) / TILE * ((m.cols + TILE - 1) / TILE)), static_cast<unsigned>(m.n));
+// tiles along the columns, along the rows (32768 at most), matrices
+dim3 tiles_of(const MxMats& m, int64_t rows, int64_t cols) {
+  return dim3(static_cast<unsigned>((m.cols + cols - 1) / cols), static_cast<unsigned>((m.rows + rows - 1) / rows), static_cast<unsigned>(m.n));
 }
 
 template <typename E, bool NOISE>
 void quantize_sides(const MxMats& m, hipStream_t st) {
+  // the images' padding along k is written too: by_row's last unit of 128 columns has two tiles
+  MxMats padded = m;
+  padded.cols = m.by_row[0] ? mx_k_units(m.cols) * MX_UNIT_K : m.cols;
+  const dim3 grid = tiles_of(padded, ROWS, COLS);
   if (m.by_row[0] && m.by_col[0])
-    k_mx_quantize<E, true, true, NOISE><<<tiles_of(m), THREADS, 0, st>>>(m);
+    k_mx_quantize<E, true, true, NOISE><<<grid, THREADS, 0, st>>>(m);
   else if (m.by_row[0])
-    k_mx_quantize<E, true, false, NOISE><<<tiles_of(m), THREADS, 0, st>>>(m);
+    k_mx_quantize<E, true, false, NOISE><<<grid, THREADS, 0, st>>>(m);
   else
-    k_mx_quantize<E, false, true, NOISE><<<tiles_of(m), THREADS, 0, st>>>(m);
+    k_mx_quantize<E, false, true, NOISE><<<grid, THREADS, 0, st>>>(m);
 }
 
 }  // namespace
@@ -289,9 +295,9 @@ hipError_t launch_mx_quantize(const MxMats& m, hipStream_t st) {
 hipError_t launch_mx_dequantize(const MxMats& m, hipStream_t st) {
   const bool col = m.by_col[0] != nullptr;
   if (m.dtype == CANZ_DT_F32)
-    col ? k_mx_dequantize<float, true><<<tiles_of(m), THREADS, 0, st>>>(m) : k_mx_dequantize<float, false><<<tiles_of(m), THREADS, 0, st>>>(m);
+    col ? k_mx_dequantize<float, true><<<tiles_of(m, TILE, TILE), THREADS, 0, st>>>(m) : k_mx_dequantize<float, false><<<tiles_of(m, TILE, TILE), THREADS, 0, st>>>(m);
   else
-    col ? k_mx_dequantize<__bf16, true><<<tiles_of(m), THREADS, 0, st>>>(m) : k_mx_dequantize<__bf16, false><<<tiles_of(m), THREADS, 0, st>>>(m);
+    col ? k_mx_dequantize<__bf16, true><<<tiles_of(m, TILE, TILE), THREADS, 0, st>>>(m) : k_mx_dequantize<__bf16, false><<<tiles_of(m, TILE, TILE), THREADS, 0, st>>>(m);
   return hipGetLastError();
 }
 
