@@ -11,6 +11,7 @@ namespace {
 
 constexpr int TILE = 128;      // rows and columns of a block's tile: whole units of codes and of scales for either image
 constexpr int THREADS = 256;
+#define CANZ_INLINE __attribute__((always_inline))
 
 typedef unsigned u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
@@ -21,6 +22,7 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 // around it, s = 2^(e - 1) with e the exponent of a, at least 0.  Adding 1.5 2^23 (s / 256) rounds a to a multiple of s / 256, ties to even, and leaves
 // that multiple in the low bits of the sum; with 2 e s added as well, bits 8 and up are the code after u is added to them.  The largest sums are those of e
 // = 2, so that one limit keeps the code at 7.
+// Returned with the code in bits 8 to 10, the sign of v in bit 11 and zeros up to bit 15.
 __device__ __forceinline__ unsigned noisy_code(float v, unsigned byte, unsigned u) {
   const float a = __builtin_amdgcn_ldexpf(__builtin_fabsf(v), 127 - static_cast<int>(byte));
   const unsigned e = max(__builtin_bit_cast(unsigned, a) >> 23, 127u);   // + 127
@@ -29,15 +31,23 @@ __device__ __forceinline__ unsigned noisy_code(float v, unsigned byte, unsigned 
   constexpr unsigned LIMIT = ((2u + 127u + 14u) << 23) + (1u << 22) + 0x7FFu;
   const float magic = __builtin_bit_cast(float, __umul24(e, STEP) + START);
   const unsigned sum = min(__builtin_bit_cast(unsigned, a + magic) + u, LIMIT);
-  return (sum >> 8 & 7u) | (__builtin_bit_cast(unsigned, v) >> 31 << 3);
+  constexpr unsigned SIGN = 1u << 11;
+  return sum | (__builtin_bit_cast(unsigned, v) >> 20 & SIGN);   // LIMIT and what the sums reach leave bit 11 free
 }
 // eight codes of one block, element 0 in the lowest bits; u: noise bytes
 template <bool NOISE>
 __device__ __forceinline__ unsigned eight_codes(const float (&v)[8], unsigned byte, const unsigned (&u)[8]) {
   unsigned r = 0;
   if constexpr (NOISE) {
+    unsigned c[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) r |= noisy_code(v[i], byte, u[i]) << (4 * i);
+    for (int i = 0; i < 8; ++i) c[i] = noisy_code(v[i], byte, u[i]);
+    // bits 8 .. 15 of four of them to the bytes of a word
+    auto gather = [](unsigned x, unsigned y, unsigned z, unsigned w) CANZ_INLINE {
+      const unsigned xy = __builtin_amdgcn_perm(y, x, 0x0C0C0501u), zw = __builtin_amdgcn_perm(w, z, 0x05010C0Cu);
+      return xy | zw;
+    };
+    r = gather(c[0], c[2], c[4], c[6]) | gather(c[1], c[3], c[5], c[7]) << 4;
   } else {
     const float s = mx_scale_value(byte);
     r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[0], v[1], s, 0);
@@ -54,6 +64,27 @@ __device__ __forceinline__ unsigned largest_of_four(unsigned v) {
   v = max(v, static_cast<unsigned>(__builtin_amdgcn_mov_dpp(static_cast<int>(v), SWAP_1, 0xF, 0xF, false)));
   return max(v, static_cast<unsigned>(__builtin_amdgcn_mov_dpp(static_cast<int>(v), SWAP_2, 0xF, 0xF, false)));
 }
+
+// Bits of the largest magnitudes of two columns (or of the even and the odd elements), gathered pair by pair: of bf16 in one register.
+template <typename E>
+struct PairMax;
+template <>
+struct PairMax<float> {
+  unsigned top[2] = {0, 0};
+  typedef float pair __attribute__((ext_vector_type(2)));
+  __device__ __forceinline__ void take(pair x) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) top[q] = max(top[q], mx_magnitude(x[q]));
+  }
+  __device__ __forceinline__ unsigned of(int q) const { return top[q]; }
+};
+template <>
+struct PairMax<__bf16> {
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  u16x2 top = {0, 0};
+  __device__ __forceinline__ void take(mx_bf16x2 x) { top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, __builtin_bit_cast(unsigned, x) & 0x7FFF7FFFu)); }
+  __device__ __forceinline__ unsigned of(int q) const { return static_cast<unsigned>(top[q]) << 16; }
+};
 
 // eight consecutive elements of a row, those behind its end as zeros
 template <typename E>
@@ -135,10 +166,10 @@ __global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {
       if constexpr (NOISE) *reinterpret_cast<uint2*>(tile_noise + row * COLS + col) = noise8;
     }
     if constexpr (ROW) {
-      unsigned amax = 0;
+      PairMax<E> top;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) amax = max(amax, mx_magnitude(v[e]));
-      const unsigned byte = mx_scale_byte(largest_of_four(amax), ceil);
+      for (int e = 0; e < 8; e += 2) top.take({static_cast<E>(v[e]), static_cast<E>(v[e + 1])});
+      const unsigned byte = mx_scale_byte(largest_of_four(max(top.of(0), top.of(1))), ceil);
       unsigned u[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) u[e] = (e < 4 ? noise8.x : noise8.y) >> (8 * (e & 3)) & 255u;
@@ -159,23 +190,20 @@ __global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {
     if (rb < ROWS / MX_BLOCK && c0 < m.cols) {
       float v[2][MX_BLOCK];
       unsigned n[MX_BLOCK];   // the noise of both
-      unsigned amax[2] = {0, 0};
+      PairMax<E> top;
 #pragma unroll
       for (int e = 0; e < MX_BLOCK; ++e) {
         const int at = (rb * MX_BLOCK + e) * COLS + c;
         const pair x = *reinterpret_cast<const pair*>(tile + at);
         n[e] = 0;
         if constexpr (NOISE) n[e] = *reinterpret_cast<const unsigned short*>(tile_noise + at);
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          v[q][e] = static_cast<float>(x[q]);
-          amax[q] = max(amax[q], mx_magnitude(v[q][e]));
-        }
+        top.take(x);
+        v[0][e] = static_cast<float>(x[0]), v[1][e] = static_cast<float>(x[1]);
       }
       const int64_t unit = mx_unit(c0 + c);
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
-        const unsigned byte = mx_scale_byte(amax[q], ceil);
+        const unsigned byte = mx_scale_byte(top.of(q), ceil);
         u32x4 codes;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
