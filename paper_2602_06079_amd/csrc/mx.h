@@ -31,11 +31,13 @@ class StreamDevice {
   hipError_t err_ = hipSuccess;
 };
 
-// Matrices of one shape in one launch.
+// Matrices of one type, width and row distance in one launch.
 constexpr int MX_MAX_MATS = 32;
 struct MxMats {
-  int64_t rows, cols, ld;
+  int64_t cols, ld;
+  int64_t most_rows;   // of all of them
   int n, dtype, scale_mode;
+  int rows[MX_MAX_MATS];
   void* mat[MX_MAX_MATS];
   uint8_t* by_row[MX_MAX_MATS];       // all null or none
   uint8_t* by_col[MX_MAX_MATS];

@@ -148,14 +148,15 @@ __global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {
   const E* const src = static_cast<const E*>(m.mat[which]);
   const uint8_t* const noise = NOISE ? m.noise[which] : nullptr;
   const int ceil = m.scale_mode == CANZ_MX_SCALE_CEIL;
-  const int64_t units_row = mx_k_units(m.cols), units_col = mx_k_units(m.rows);   // k units of the two images
+  const int64_t rows = m.rows[which], units_row = mx_k_units(m.cols), units_col = mx_k_units(rows);   // units along k of the two images
+  if (r0 >= rows) return;   // a matrix of fewer rows than others of the launch
   const int kb0 = static_cast<int>(c0 / MX_BLOCK) & 3;                            // 0 or 2: the tile is one half of a k unit of by_row
 
   const int col = (t & 7) * 8;
 #pragma unroll
   for (int i = 0; i < ROWS / 32; ++i) {
     const int row = i * 32 + (t >> 3);
-    const int64_t left = r0 + row < m.rows ? m.cols - (c0 + col) : 0;
+    const int64_t left = r0 + row < rows ? m.cols - (c0 + col) : 0;
     float v[8];
     load8(src + (r0 + row) * m.ld + c0 + col, left, v);
     uint2 noise8 = {0, 0};
@@ -176,7 +177,7 @@ __global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {
       const unsigned codes = eight_codes<NOISE>(v, byte, u);
       const int kb = (t & 7) >> 2;
       const int64_t unit = mx_unit(r0 + row);
-      if (unit < mx_row_tiles(m.rows))
+      if (unit < mx_row_tiles(rows))
         *reinterpret_cast<unsigned*>(m.by_row[which] + (unit * units_row + c0 / MX_UNIT_K) * MX_UNIT_BYTES + ((kb0 + kb) * 16 + mx_slot(row)) * 16 +
                                      (t & 3) * 4) = codes;
       if ((t & 3) == 0) reinterpret_cast<uint8_t*>(&row_scales[row >> 6][kb][mx_slot(row)])[mx_unit(row) % 4] = static_cast<uint8_t>(byte);
@@ -220,11 +221,11 @@ __global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {
     __syncthreads();
   }
   const int half = t >> 5 & 1, word = t & 31;
-  if (ROW && t < 64 && r0 + half * MX_PAD_ROWS < m.rows)
-    *reinterpret_cast<unsigned*>(m.by_row[which] + mx_code_bytes(m.rows, m.cols) +
+  if (ROW && t < 64 && r0 + half * MX_PAD_ROWS < rows)
+    *reinterpret_cast<unsigned*>(m.by_row[which] + mx_code_bytes(rows, m.cols) +
                                  ((r0 / MX_PAD_ROWS + half) * units_row + c0 / MX_UNIT_K) * MX_SCALE_BYTES + (kb0 * 16 + word) * 4) = row_scales[half][word >> 4][word & 15];
   if (COL && t >= 64 && t < 128 && c0 < m.cols)
-    *reinterpret_cast<unsigned*>(m.by_col[which] + mx_code_bytes(m.cols, m.rows) +
+    *reinterpret_cast<unsigned*>(m.by_col[which] + mx_code_bytes(m.cols, rows) +
                                  (c0 / MX_PAD_ROWS * units_col + r0 / MX_UNIT_K) * MX_SCALE_BYTES + (t - 64) * 4) = col_scales[(t - 64) >> 4][t & 15];
 }
 
@@ -246,9 +247,10 @@ __global__ __launch_bounds__(THREADS) void k_mx_dequantize(MxMats m) {
   const int t = threadIdx.x, which = blockIdx.z;
   const int64_t r0 = static_cast<int64_t>(blockIdx.y) * TILE, c0 = static_cast<int64_t>(blockIdx.x) * TILE;
   E* const dst = static_cast<E*>(m.mat[which]);
+  const int64_t rows = m.rows[which];
   if constexpr (COL) {
     const uint8_t* const img = m.by_col[which];
-    const int64_t units = mx_k_units(m.rows), ks = r0 / MX_UNIT_K;
+    const int64_t units = mx_k_units(rows), ks = r0 / MX_UNIT_K;
     const int c = t & (TILE - 1);
     const int64_t unit = mx_unit(c0 + c);
     if (c0 + c < m.cols) {
@@ -256,7 +258,7 @@ __global__ __launch_bounds__(THREADS) void k_mx_dequantize(MxMats m) {
       for (int i = 0; i < 2; ++i) {
         const int rb = (t >> 7) + 2 * i;
         const u32x4 codes = *reinterpret_cast<const u32x4*>(img + (unit * units + ks) * MX_UNIT_BYTES + (rb * 16 + mx_slot(c)) * 16);
-        const unsigned byte = img[mx_code_bytes(m.cols, m.rows) + (unit / 4 * units + ks) * MX_SCALE_BYTES + (rb * 16 + mx_slot(c)) * 4 + unit % 4];
+        const unsigned byte = img[mx_code_bytes(m.cols, rows) + (unit / 4 * units + ks) * MX_SCALE_BYTES + (rb * 16 + mx_slot(c)) * 4 + unit % 4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           float v[8];
@@ -274,7 +276,7 @@ __global__ __launch_bounds__(THREADS) void k_mx_dequantize(MxMats m) {
 #pragma unroll 4
   for (int i = 0; i < TILE / 16; ++i) {
     const int row = i * 16 + (t >> 4);
-    if (r0 + row >= m.rows) break;
+    if (r0 + row >= rows) break;
     float v[8];
     if constexpr (COL) {
 #pragma unroll
@@ -284,7 +286,7 @@ __global__ __launch_bounds__(THREADS) void k_mx_dequantize(MxMats m) {
       const int64_t units = mx_k_units(m.cols), ks = c0 / MX_UNIT_K, unit = mx_unit(r0 + row);
       const int at = ((t & 15) >> 2) * 16 + mx_slot(row);
       const unsigned codes = *reinterpret_cast<const unsigned*>(img + (unit * units + ks) * MX_UNIT_BYTES + at * 16 + (t & 3) * 4);
-      const unsigned byte = img[mx_code_bytes(m.rows, m.cols) + (unit / 4 * units + ks) * MX_SCALE_BYTES + at * 4 + unit % 4];
+      const unsigned byte = img[mx_code_bytes(rows, m.cols) + (unit / 4 * units + ks) * MX_SCALE_BYTES + at * 4 + unit % 4];
       eight_values(codes, byte, v);
     }
     store8(dst + (r0 + row) * m.ld + c0 + col, left, v);
@@ -293,7 +295,7 @@ __global__ __launch_bounds__(THREADS) void k_mx_dequantize(MxMats m) {
 
 // tiles along the columns, along the rows (32768 at most), matrices
 dim3 tiles_of(const MxMats& m, int64_t rows, int64_t cols) {
-  return dim3(static_cast<unsigned>((m.cols + cols - 1) / cols), static_cast<unsigned>((m.rows + rows - 1) / rows), static_cast<unsigned>(m.n));
+  return dim3(static_cast<unsigned>((m.cols + cols - 1) / cols), static_cast<unsigned>((m.most_rows + rows - 1) / rows), static_cast<unsigned>(m.n));
 }
 
 template <typename E, bool NOISE>

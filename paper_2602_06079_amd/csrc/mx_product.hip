@@ -384,7 +384,8 @@ __device__ __forceinline__ Tile tile_at(KernArgs ps, int logical) {
   return Tile{j, (band * BAND + in_band - tn * rows) * 2 * W, tn * 2 * W};
 }
 
-template <int W, typename E, bool BETA>
+// ONLY, ONLY_BETA: the type of the results and whether old ones are read; void: as each product says
+template <int W, typename ONLY, bool ONLY_BETA>
 __global__ __launch_bounds__(THREADS, W == 8 ? 1 : 2) void k_mx_product(MxProblems) {
   using S = Stage<W>;
   const KernArgs ps = (KernArgs)__builtin_amdgcn_kernarg_segment_ptr();
@@ -495,7 +496,9 @@ __global__ __launch_bounds__(THREADS, W == 8 ? 1 : 2) void k_mx_product(MxProble
     });
   };
 
-  auto store_tile = [&](const Tile& t) CANZ_INLINE {
+  auto store_tile = [&](const Tile& t, auto type, auto reads) CANZ_INLINE {
+    using E = std::remove_pointer_t<decltype(type)>;
+    constexpr bool BETA = decltype(reads)::value;
     int lane = threadIdx.x & 63;   // opaque, or every address that depends on it is kept across the tiles
     asm volatile("" : "+v"(lane));
     const int64_t rows = ps->pr[t.problem].m, ldc = ps->pr[t.problem].ldc;
@@ -582,7 +585,21 @@ __global__ __launch_bounds__(THREADS, W == 8 ? 1 : 2) void k_mx_product(MxProble
       step(Set0{}, st2, st3, load_u + 2);
       step(Set1{}, st3, st0, load_u + 3);
     }
-    store_tile(t);
+    if constexpr (!std::is_void_v<ONLY>) {
+      store_tile(t, static_cast<ONLY*>(nullptr), std::bool_constant<ONLY_BETA>{});
+    } else {
+      const bool reads = ps->pr[t.problem].beta != 0.f;
+      auto as = [&](auto type) CANZ_INLINE {
+        if (reads)
+          store_tile(t, type, std::true_type{});
+        else
+          store_tile(t, type, std::false_type{});
+      };
+      if (ps->pr[t.problem].out_dtype == CANZ_DT_F32)
+        as(static_cast<float*>(nullptr));
+      else
+        as(static_cast<__bf16*>(nullptr));
+    }
   }
   __builtin_amdgcn_s_waitcnt(wait_code(0));   // the requests behind the last tile have landed before the block leaves
 }
@@ -611,16 +628,30 @@ int64_t small_tiles_ns(int64_t tiles, int64_t ks) {
 }
 
 template <typename E, bool BETA>
+void launch_large_tiles(const MxProblems& all, hipStream_t st) {
+  MxProblems ps;
+  ps.n = 0;
+  for (int i = 0; i < all.n; ++i)
+    if ((all.pr[i].out_dtype == CANZ_DT_F32) == (sizeof(E) == 4) && (all.pr[i].beta != 0.f) == BETA) ps.pr[ps.n++] = all.pr[i];
+  if (ps.n == 0) return;
+  const int64_t tiles = count_tiles(ps, 256, 256);
+  k_mx_product<8, E, BETA><<<dim3(static_cast<unsigned>(std::min<int64_t>(tiles, N_CU))), THREADS, 0, st>>>(ps);
+}
+
+// All products in one launch of small tiles, or in one of large tiles for each type of result (a large tile's epilogue is too much code
+// to have it in a kernel four times).
 hipError_t launch_tiles(MxProblems& ps, hipStream_t st) {
   const int64_t large = count_tiles(ps, 256, 256), small = count_tiles(ps, 128, 128);
   int64_t units = 0;   // of all small tiles along k
   for (int i = 0; i < ps.n; ++i) units += ((i + 1 < ps.n ? ps.pr[i + 1].first_tile : small) - ps.pr[i].first_tile) * mx_k_units(ps.pr[i].k);
   const int64_t ks = (units + small - 1) / small;
   if (large_tiles_ns(large, ks) < small_tiles_ns(small, ks)) {
-    count_tiles(ps, 256, 256);
-    k_mx_product<8, E, BETA><<<dim3(static_cast<unsigned>(std::min<int64_t>(large, N_CU))), THREADS, 0, st>>>(ps);
+    launch_large_tiles<float, false>(ps, st);
+    launch_large_tiles<__bf16, false>(ps, st);
+    launch_large_tiles<float, true>(ps, st);
+    launch_large_tiles<__bf16, true>(ps, st);
   } else {
-    k_mx_product<4, E, BETA><<<dim3(static_cast<unsigned>(std::min<int64_t>(small, 2 * N_CU))), THREADS, 0, st>>>(ps);
+    k_mx_product<4, void, false><<<dim3(static_cast<unsigned>(std::min<int64_t>(small, 2 * N_CU))), THREADS, 0, st>>>(ps);
   }
   return hipGetLastError();
 }
@@ -651,14 +682,14 @@ hipError_t launch_few(MxProblems& ps, Width width, hipStream_t st) {
 }
 
 // The launches that a product may be part of.
-enum Kind { SCALE, TILES, IMAGE_16 = TILES + 4, IMAGE_32 = IMAGE_16 + WIDTHS, IMAGE_64 = IMAGE_32 + WIDTHS, ROUND_BF16 = IMAGE_64 + WIDTHS,
+enum Kind { SCALE, TILES, IMAGE_16, IMAGE_32 = IMAGE_16 + WIDTHS, IMAGE_64 = IMAGE_32 + WIDTHS, ROUND_BF16 = IMAGE_64 + WIDTHS,
             ROUND_F32 = ROUND_BF16 + WIDTHS, KINDS = ROUND_F32 + WIDTHS };
 int kind_of(const MxProblem& p) {
   if (p.k == 0) return SCALE;
   const Width w = width_of(p.n);
   if (p.a_dtype != CANZ_DT_MX) return (p.a_dtype == CANZ_DT_BF16 ? ROUND_BF16 : ROUND_F32) + w;
   if (p.m <= FEW_ROWS) return (p.m <= 16 ? IMAGE_16 : p.m <= 32 ? IMAGE_32 : IMAGE_64) + w;
-  return TILES + (p.out_dtype == CANZ_DT_F32 ? 0 : 1) + (p.beta != 0.f ? 2 : 0);
+  return TILES;
 }
 
 hipError_t launch_kind(int kind, MxProblems& ps, hipStream_t st) {
@@ -670,10 +701,7 @@ hipError_t launch_kind(int kind, MxProblems& ps, hipStream_t st) {
         err = hipGetLastError();
       }
       return err;
-    case TILES: return launch_tiles<float, false>(ps, st);
-    case TILES + 1: return launch_tiles<__bf16, false>(ps, st);
-    case TILES + 2: return launch_tiles<float, true>(ps, st);
-    case TILES + 3: return launch_tiles<__bf16, true>(ps, st);
+    case TILES: return launch_tiles(ps, st);
     default: break;
   }
   const Width w = static_cast<Width>((kind - IMAGE_16) % WIDTHS);

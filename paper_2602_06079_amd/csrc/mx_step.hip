@@ -40,10 +40,11 @@ int for_each_launch(const canz_mx_group& g, int scale_mode, bool noise, F&& fn) 
   if (g.rows == 0 || g.cols == 0) return CANZ_OK;
   for (int first = 0; first < g.n_mats; first += MX_MAX_MATS) {
     MxMats m{};
-    m.rows = g.rows, m.cols = g.cols, m.ld = g.ld;
+    m.most_rows = g.rows, m.cols = g.cols, m.ld = g.ld;
     m.n = std::min(MX_MAX_MATS, g.n_mats - first);
     m.dtype = g.dtype, m.scale_mode = scale_mode;
     for (int i = 0; i < m.n; ++i) {
+      m.rows[i] = static_cast<int>(g.rows);
       m.mat[i] = g.mat[first + i];
       m.by_row[i] = g.by_row ? static_cast<uint8_t*>(g.by_row[first + i]) : nullptr;
       m.by_col[i] = g.by_col ? static_cast<uint8_t*>(g.by_col[first + i]) : nullptr;
@@ -173,38 +174,49 @@ extern "C" int canz_mx_product(const canz_mx_product_group* g, int32_t n_groups,
   const StreamDevice on(st);
   if (on.error() != hipSuccess) return fail(CANZ_EHIP, "stream: %s", hipGetErrorString(on.error()));
 
-  uint8_t* ws = static_cast<uint8_t*>(workspace);
-  MxProblems ps;
-  ps.n = 0;
-  auto flush = [&]() {
-    const hipError_t err = launch_mx_product(ps, st);
-    ps.n = 0;
+  // images of the matrices that are rounded before: those of one width, type and rule in one launch, whatever their rows (experts)
+  uint8_t* const images = static_cast<uint8_t*>(workspace);
+  size_t at = 0;
+  MxMats mats{};
+  auto round = [&]() -> int {
+    if (mats.n == 0) return CANZ_OK;
+    const hipError_t err = launch_mx_quantize(mats, st);
+    mats.n = 0;
     return err == hipSuccess ? CANZ_OK : fail(CANZ_EHIP, "microscaled product: %s", hipGetErrorString(err));
   };
   for (int i = 0; i < n_groups; ++i) {
     const canz_mx_product_group& gi = g[i];
-    if (mx_idle(gi)) continue;
-    uint8_t* const images = ws;
-    const size_t each = static_cast<size_t>(mx_image_bytes(gi.m, gi.k));
-    const bool before = mx_rounded_before(gi);
-    if (before) {
-      for (int first = 0; first < gi.n_prods; first += MX_MAX_MATS) {
-        MxMats m{};
-        m.rows = gi.m, m.cols = gi.k, m.ld = gi.lda;
-        m.n = std::min(MX_MAX_MATS, gi.n_prods - first);
-        m.dtype = gi.a_dtype, m.scale_mode = gi.a_scale_mode;
-        for (int x = 0; x < m.n; ++x) {
-          m.mat[x] = const_cast<void*>(gi.a[first + x]);
-          m.by_row[x] = images + (first + x) * each;
-        }
-        const hipError_t err = launch_mx_quantize(m, st);
-        if (err != hipSuccess) return fail(CANZ_EHIP, "microscaled product: %s", hipGetErrorString(err));
-      }
-      ws += gi.n_prods * each;
+    if (!mx_rounded_before(gi)) continue;
+    for (int x = 0; x < gi.n_prods; ++x) {
+      const bool alike = mats.cols == gi.k && mats.ld == gi.lda && mats.dtype == gi.a_dtype && mats.scale_mode == gi.a_scale_mode;
+      if (mats.n == MX_MAX_MATS || !alike)
+        if (int rc = round()) return rc;
+      if (mats.n == 0) mats.cols = gi.k, mats.ld = gi.lda, mats.dtype = gi.a_dtype, mats.scale_mode = gi.a_scale_mode, mats.most_rows = 0;
+      mats.most_rows = std::max(mats.most_rows, gi.m);
+      mats.rows[mats.n] = static_cast<int>(gi.m);
+      mats.mat[mats.n] = const_cast<void*>(gi.a[x]);
+      mats.by_row[mats.n++] = images + at;
+      at += static_cast<size_t>(mx_image_bytes(gi.m, gi.k));
     }
+  }
+  if (int rc = round()) return rc;
+
+  MxProblems ps;
+  ps.n = 0;
+  auto flush = [&]() -> int {
+    const hipError_t err = launch_mx_product(ps, st);
+    ps.n = 0;
+    return err == hipSuccess ? CANZ_OK : fail(CANZ_EHIP, "microscaled product: %s", hipGetErrorString(err));
+  };
+  at = 0;
+  for (int i = 0; i < n_groups; ++i) {
+    const canz_mx_product_group& gi = g[i];
+    if (mx_idle(gi)) continue;
+    const bool before = mx_rounded_before(gi);
     for (int x = 0; x < gi.n_prods; ++x) {
       MxProblem& p = ps.pr[ps.n++];
-      p.a = before ? images + x * each : static_cast<const uint8_t*>(gi.k > 0 ? gi.a[x] : nullptr);
+      p.a = before ? images + at : static_cast<const uint8_t*>(gi.k > 0 ? gi.a[x] : nullptr);
+      if (before) at += static_cast<size_t>(mx_image_bytes(gi.m, gi.k));
       p.a_dtype = before ? CANZ_DT_MX : gi.a_dtype, p.a_ceil = gi.a_scale_mode == CANZ_MX_SCALE_CEIL, p.lda = gi.lda;
       p.b = static_cast<const uint8_t*>(gi.k > 0 ? gi.b[x] : nullptr);
       p.c = gi.c[x];
