@@ -372,16 +372,27 @@ struct Tile {
   int problem;   // -1: none
   int m0, n0;    // in units of 16 rows
 };
+// Number `logical` of the launch's tiles.  Every XCD (blockIdx % 8, and logical % 8, since a grid has a multiple of 8 blocks or no second round) has an
+// eighth of each product, in one piece: what its blocks work on at a time is a patch of neighbours that share operands in its L2, and products of
+// unequal length burden all XCDs alike.
 template <int W>
 __device__ __forceinline__ Tile tile_at(KernArgs ps, int logical) {
-  if (logical >= ps->tiles) return Tile{-1, 0, 0};
-  int j = 0;
-  while (j + 1 < ps->n && logical >= ps->pr[j + 1].first_tile) ++j;
-  const int tix = logical - ps->pr[j].first_tile;
-  const int tiles_m = static_cast<int>((ps->pr[j].m + 32 * W - 1) / (32 * W)), tiles_n = static_cast<int>((ps->pr[j].n + 32 * W - 1) / (32 * W));
-  const int band = tix / (BAND * tiles_n), in_band = tix - band * BAND * tiles_n, rows = min(BAND, tiles_m - band * BAND);
-  const int tn = in_band / rows;
-  return Tile{j, (band * BAND + in_band - tn * rows) * 2 * W, tn * 2 * W};
+  const int xcd = logical % N_XCD;
+  int q = logical / N_XCD;
+  for (int j = 0; j < ps->n; ++j) {
+    const int tiles = (j + 1 < ps->n ? ps->pr[j + 1].first_tile : ps->tiles) - ps->pr[j].first_tile;
+    const int begin = tiles * xcd / N_XCD, count = tiles * (xcd + 1) / N_XCD - begin;
+    if (q >= count) {
+      q -= count;
+      continue;
+    }
+    const int tix = begin + q;
+    const int tiles_m = static_cast<int>((ps->pr[j].m + 32 * W - 1) / (32 * W)), tiles_n = static_cast<int>((ps->pr[j].n + 32 * W - 1) / (32 * W));
+    const int band = tix / (BAND * tiles_n), in_band = tix - band * BAND * tiles_n, rows = min(BAND, tiles_m - band * BAND);
+    const int tn = in_band / rows;
+    return Tile{j, (band * BAND + in_band - tn * rows) * 2 * W, tn * 2 * W};
+  }
+  return Tile{-1, 0, 0};
 }
 
 // ONLY, ONLY_BETA: the type of the results and whether old ones are read; void: as each product says
@@ -397,13 +408,13 @@ __global__ __launch_bounds__(THREADS, W == 8 ? 1 : 2) void k_mx_product(MxProble
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1;
 
-  const int slot = xcd_slot();   // in every round the blocks of an XCD have a patch of tiles
+  if (tile_at<W>(ps, blockIdx.x).problem < 0) return;   // this XCD's share is one tile less
 
   // ---- loading: this wavefront's pieces of the next four stages.  Every tile takes whole rounds of the ring, so its loop has no exit
   // inside and the accumulators stay where they are; units behind the last one are asked for in an empty buffer, which gives zeros.
   // Through buffer descriptors (of the tile's codes and scales of either operand) a load is one instruction beside its LDS address: the piece is the
   // lane's offset, the unit a scalar one.
-  int next_logical = slot, load_u = 0, load_ks = 0;
+  int next_logical = blockIdx.x, load_u = 0, load_ks = 0;
   const uint8_t *code_base[2], *scale_base[2];   // of A and B, from the tile's first unit on
   unsigned code_room[2], scale_room[2];          // bytes there
   int code_off[W], scale_off[S::scale_loads];    // this lane's part of its pieces
@@ -571,7 +582,7 @@ __global__ __launch_bounds__(THREADS, W == 8 ? 1 : 2) void k_mx_product(MxProble
   CANZ_FENCE();
   static_for<READS>([&](auto idx) CANZ_INLINE { read_one(st0, 0, idx); });
 
-  for (int logical = slot;; logical += gridDim.x) {
+  for (int logical = blockIdx.x;; logical += gridDim.x) {
     const Tile t = tile_at<W>(ps, logical);
     if (t.problem < 0) break;
 #pragma unroll
@@ -627,6 +638,13 @@ int64_t small_tiles_ns(int64_t tiles, int64_t ks) {
   return tiles / (2 * N_CU) * (460 * ks + 2600) + (rest > N_CU ? 460 * ks + 2600 : rest > 0 ? 210 * ks + 2600 : 0);
 }
 
+// blocks for these tiles, `most` (a multiple of 8) at a time: as many on each XCD as the one with most tiles has
+dim3 tile_grid(const MxProblems& ps, int64_t tiles, int most) {
+  int64_t longest = 0;   // an XCD has at most an eighth of each product, rounded up
+  for (int i = 0; i < ps.n; ++i) longest += ((i + 1 < ps.n ? ps.pr[i + 1].first_tile : tiles) - ps.pr[i].first_tile + N_XCD - 1) / N_XCD;
+  return dim3(static_cast<unsigned>(std::min<int64_t>(N_XCD * longest, most)));
+}
+
 template <typename E, bool BETA>
 void launch_large_tiles(const MxProblems& all, hipStream_t st) {
   MxProblems ps;
@@ -635,12 +653,13 @@ void launch_large_tiles(const MxProblems& all, hipStream_t st) {
     if ((all.pr[i].out_dtype == CANZ_DT_F32) == (sizeof(E) == 4) && (all.pr[i].beta != 0.f) == BETA) ps.pr[ps.n++] = all.pr[i];
   if (ps.n == 0) return;
   const int64_t tiles = count_tiles(ps, 256, 256);
-  k_mx_product<8, E, BETA><<<dim3(static_cast<unsigned>(std::min<int64_t>(tiles, N_CU))), THREADS, 0, st>>>(ps);
+  k_mx_product<8, E, BETA><<<tile_grid(ps, tiles, N_CU), THREADS, 0, st>>>(ps);
 }
 
 // All products in one launch of small tiles, or in one of large tiles for each type of result (a large tile's epilogue is too much code
 // to have it in a kernel four times).
 hipError_t launch_tiles(MxProblems& ps, hipStream_t st) {
+  std::sort(ps.pr, ps.pr + ps.n, [](const MxProblem& x, const MxProblem& y) { return x.k > y.k; });   // the longest begin
   const int64_t large = count_tiles(ps, 256, 256), small = count_tiles(ps, 128, 128);
   int64_t units = 0;   // of all small tiles along k
   for (int i = 0; i < ps.n; ++i) units += ((i + 1 < ps.n ? ps.pr[i + 1].first_tile : small) - ps.pr[i].first_tile) * mx_k_units(ps.pr[i].k);
@@ -651,7 +670,7 @@ hipError_t launch_tiles(MxProblems& ps, hipStream_t st) {
     launch_large_tiles<float, true>(ps, st);
     launch_large_tiles<__bf16, true>(ps, st);
   } else {
-    k_mx_product<4, void, false><<<dim3(static_cast<unsigned>(std::min<int64_t>(small, 2 * N_CU))), THREADS, 0, st>>>(ps);
+    k_mx_product<4, void, false><<<tile_grid(ps, small, 2 * N_CU), THREADS, 0, st>>>(ps);
   }
   return hipGetLastError();
 }
