@@ -57,15 +57,31 @@ struct MxProblem {
   int64_t m, n, k, lda, ldc;
   float alpha, beta;
   int a_dtype, a_ceil, out_dtype;
-  int first_tile;   // set by the launcher
+  int first_unit, units;   // the part of k that is multiplied (images of more than 64 rows), in units of 128
 };
 constexpr int MX_MAX_PROBLEMS = 32;
+
+// How many parts k is cut into, each a problem of its own with fp32 sums in the workspace, which launch_mx_join adds up: products of more than 64 rows whose
+// tiles leave most of the chip idle for long.  A unit takes a tile 210 ns, the join about 5 us: us, whole and in parts: 100 x 1000 x 20000 35.5 and JOIN_A,
+// 512 x 512 x 8192 JOIN_B.  A product alone decides, so that its sums do not depend on what shares the call.
+constexpr int MX_MAX_PARTS = 8;
+constexpr int mx_parts(int64_t m, int64_t n, int64_t k) {
+  if (m <= 64 || n == 0 || k == 0) return 1;
+  const int64_t tiles = ((m + 127) / 128) * ((n + 127) / 128), units = mx_k_units(k);
+  int64_t parts = 128 / tiles;
+  if (parts > MX_MAX_PARTS) parts = MX_MAX_PARTS;
+  if (parts > units / 8) parts = units / 8;
+  return parts >= 2 && (units - units / parts) * 210 >= 8000 ? static_cast<int>(parts) : 1;
+}
 struct MxProblems {
   int n;
-  int tiles;        // of all problems, set by the launcher
+  int first_tile[MX_MAX_PROBLEMS + 1];   // of every problem, then their number: set by the launcher, side by side, since every block goes through them
   MxProblem pr[MX_MAX_PROBLEMS];
 };
 hipError_t launch_mx_product(const MxProblems& p, hipStream_t st);
+
+// C = alpha (sum of `parts` matrices of m x n fp32 sums, one behind the other) + beta C
+hipError_t launch_mx_join(const MxProblem& p, const float* sums, int parts, hipStream_t st);
 
 // Validates one group of canz_mx_quantize (`back`: of canz_mx_dequantize).
 int check_mx_group(const canz_mx_group& g, int idx, bool back);

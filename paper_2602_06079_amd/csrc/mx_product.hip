@@ -187,9 +187,9 @@ __global__ __launch_bounds__(64 * WAVES) void k_mx_product_few(MxProblems) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int slot = xcd_slot();
   int j = 0;
-  while (j + 1 < ps->n && slot >= ps->pr[j + 1].first_tile) ++j;
+  while (slot >= ps->first_tile[j + 1]) ++j;
   const int64_t m = ps->pr[j].m, n = ps->pr[j].n, k = ps->pr[j].k, lda = ps->pr[j].lda;
-  const int64_t part = slot - ps->pr[j].first_tile;   // of B
+  const int64_t part = slot - ps->first_tile[j];   // of B
   const int ks = static_cast<int>(mx_k_units(k));
   const uint8_t* const bc = ps->pr[j].b + part * UN * ks * MX_UNIT_BYTES + lane * 16;
   const uint8_t* const bs = ps->pr[j].b + mx_code_bytes(n, k) + part * UN / 4 * ks * MX_SCALE_BYTES + lane * 4;
@@ -334,6 +334,28 @@ __global__ __launch_bounds__(64 * WAVES) void k_mx_product_few(MxProblems) {
   }
 }
 
+// ---- sums of parts of k -------------------------------------------------------------------------------------------------------
+__global__ __launch_bounds__(THREADS) void k_mx_join(MxProblem p, const float* sums, int parts) {
+  const int64_t total = p.m * p.n;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * THREADS + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * THREADS) {
+    float part[MX_MAX_PARTS];
+#pragma unroll
+    for (int q = 0; q < MX_MAX_PARTS; ++q) part[q] = q < parts ? sums[q * total + i] : 0.f;   // all on their way before the first is added
+    float v = part[0];
+#pragma unroll
+    for (int q = 1; q < MX_MAX_PARTS; ++q) v += part[q];
+    v *= p.alpha;
+    const int64_t at = i / p.n * p.ldc + i % p.n;
+    if (p.out_dtype == CANZ_DT_F32) {
+      float* const c = static_cast<float*>(p.c) + at;
+      *c = p.beta != 0.f ? __builtin_fmaf(p.beta, *c, v) : v;
+    } else {
+      __bf16* const c = static_cast<__bf16*>(p.c) + at;
+      *c = static_cast<__bf16>(p.beta != 0.f ? __builtin_fmaf(p.beta, static_cast<float>(*c), v) : v);
+    }
+  }
+}
+
 // ---- nothing along k: C <- beta C ---------------------------------------------------------------------------------------------
 __global__ __launch_bounds__(THREADS) void k_mx_scale(MxProblem p) {
   const int64_t total = p.m * p.n;
@@ -380,7 +402,7 @@ __device__ __forceinline__ Tile tile_at(KernArgs ps, int logical) {
   const int xcd = logical % N_XCD;
   int q = logical / N_XCD;
   for (int j = 0; j < ps->n; ++j) {
-    const int tiles = (j + 1 < ps->n ? ps->pr[j + 1].first_tile : ps->tiles) - ps->pr[j].first_tile;
+    const int tiles = ps->first_tile[j + 1] - ps->first_tile[j];
     const int begin = tiles * xcd / N_XCD, count = tiles * (xcd + 1) / N_XCD - begin;
     if (q >= count) {
       q -= count;
@@ -408,26 +430,25 @@ __global__ __launch_bounds__(THREADS, W == 8 ? 1 : 2) void k_mx_product(MxProble
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1;
 
-  if (tile_at<W>(ps, blockIdx.x).problem < 0) return;   // this XCD's share is one tile less
-
   // ---- loading: this wavefront's pieces of the next four stages.  Every tile takes whole rounds of the ring, so its loop has no exit
   // inside and the accumulators stay where they are; units behind the last one are asked for in an empty buffer, which gives zeros.
   // Through buffer descriptors (of the tile's codes and scales of either operand) a load is one instruction beside its LDS address: the piece is the
   // lane's offset, the unit a scalar one.
-  int next_logical = blockIdx.x, load_u = 0, load_ks = 0;
+  Tile next_tile;   // the one that is loaded: the next one, from the last round of a tile on
+  int next_logical = blockIdx.x, load_u = 0, load_ks = 0;        // load_ks: the end of the product's part of k
   const uint8_t *code_base[2], *scale_base[2];   // of A and B, from the tile's first unit on
   unsigned code_room[2], scale_room[2];          // bytes there
   int code_off[W], scale_off[S::scale_loads];    // this lane's part of its pieces
   auto next_round = [&]() CANZ_INLINE {
     load_u += 4;
     if (load_u < load_ks) return;
-    load_u = 0;
-    const Tile t = tile_at<W>(ps, next_logical);
+    const Tile t = next_tile = tile_at<W>(ps, next_logical);
     load_ks = 0;
     if (t.problem < 0) return;   // nothing left: zeros
     next_logical += gridDim.x;
-    load_ks = static_cast<int>(mx_k_units(ps->pr[t.problem].k));
-    const int row_bytes = load_ks * MX_UNIT_BYTES, scale_bytes = load_ks * MX_SCALE_BYTES;   // 2^25 at most
+    load_u = ps->pr[t.problem].first_unit, load_ks = load_u + ps->pr[t.problem].units;
+    const int ks = static_cast<int>(mx_k_units(ps->pr[t.problem].k));
+    const int row_bytes = ks * MX_UNIT_BYTES, scale_bytes = ks * MX_SCALE_BYTES;   // 2^25 at most
     int there[2];   // units of the tile that the image has
 #pragma unroll
     for (int o = 0; o < 2; ++o) {
@@ -573,6 +594,7 @@ __global__ __launch_bounds__(THREADS, W == 8 ? 1 : 2) void k_mx_product(MxProble
   using Set0 = std::integral_constant<int, 0>;
   using Set1 = std::integral_constant<int, 1>;
   next_round();
+  if (next_tile.problem < 0) return;   // this XCD's share is one tile less than others'
   static_for<S::loads>([&](auto idx) CANZ_INLINE { fetch_one(st0, load_u, idx); });
   static_for<S::loads>([&](auto idx) CANZ_INLINE { fetch_one(st1, load_u + 1, idx); });
   static_for<S::loads>([&](auto idx) CANZ_INLINE { fetch_one(st2, load_u + 2, idx); });
@@ -582,14 +604,14 @@ __global__ __launch_bounds__(THREADS, W == 8 ? 1 : 2) void k_mx_product(MxProble
   CANZ_FENCE();
   static_for<READS>([&](auto idx) CANZ_INLINE { read_one(st0, 0, idx); });
 
-  for (int logical = blockIdx.x;; logical += gridDim.x) {
-    const Tile t = tile_at<W>(ps, logical);
+  for (;;) {
+    const Tile t = next_tile;
     if (t.problem < 0) break;
 #pragma unroll
     for (int i = 0; i < W; ++i)
 #pragma unroll
       for (int j = 0; j < W; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int rounds = static_cast<int>((mx_k_units(ps->pr[t.problem].k) + 3) / 4); rounds > 0; --rounds) {
+    for (int rounds = (ps->pr[t.problem].units + 3) / 4; rounds > 0; --rounds) {
       next_round();
       step(Set0{}, st0, st1, load_u);
       step(Set1{}, st1, st2, load_u + 1);
@@ -619,10 +641,10 @@ __global__ __launch_bounds__(THREADS, W == 8 ? 1 : 2) void k_mx_product(MxProble
 int64_t count_tiles(MxProblems& ps, int rows, int cols) {
   int64_t tiles = 0;
   for (int i = 0; i < ps.n; ++i) {
-    ps.pr[i].first_tile = static_cast<int>(tiles);
+    ps.first_tile[i] = static_cast<int>(tiles);
     tiles += (ps.pr[i].m + rows - 1) / rows * ((ps.pr[i].n + cols - 1) / cols);
   }
-  ps.tiles = static_cast<int>(tiles);
+  ps.first_tile[ps.n] = static_cast<int>(tiles);
   return tiles;
 }
 
@@ -639,9 +661,9 @@ int64_t small_tiles_ns(int64_t tiles, int64_t ks) {
 }
 
 // blocks for these tiles, `most` (a multiple of 8) at a time: as many on each XCD as the one with most tiles has
-dim3 tile_grid(const MxProblems& ps, int64_t tiles, int most) {
+dim3 tile_grid(const MxProblems& ps, int most) {
   int64_t longest = 0;   // an XCD has at most an eighth of each product, rounded up
-  for (int i = 0; i < ps.n; ++i) longest += ((i + 1 < ps.n ? ps.pr[i + 1].first_tile : tiles) - ps.pr[i].first_tile + N_XCD - 1) / N_XCD;
+  for (int i = 0; i < ps.n; ++i) longest += (ps.first_tile[i + 1] - ps.first_tile[i] + N_XCD - 1) / N_XCD;
   return dim3(static_cast<unsigned>(std::min<int64_t>(N_XCD * longest, most)));
 }
 
@@ -652,17 +674,17 @@ void launch_large_tiles(const MxProblems& all, hipStream_t st) {
   for (int i = 0; i < all.n; ++i)
     if ((all.pr[i].out_dtype == CANZ_DT_F32) == (sizeof(E) == 4) && (all.pr[i].beta != 0.f) == BETA) ps.pr[ps.n++] = all.pr[i];
   if (ps.n == 0) return;
-  const int64_t tiles = count_tiles(ps, 256, 256);
-  k_mx_product<8, E, BETA><<<tile_grid(ps, tiles, N_CU), THREADS, 0, st>>>(ps);
+  count_tiles(ps, 256, 256);
+  k_mx_product<8, E, BETA><<<tile_grid(ps, N_CU), THREADS, 0, st>>>(ps);
 }
 
 // All products in one launch of small tiles, or in one of large tiles for each type of result (a large tile's epilogue is too much code
 // to have it in a kernel four times).
 hipError_t launch_tiles(MxProblems& ps, hipStream_t st) {
-  std::sort(ps.pr, ps.pr + ps.n, [](const MxProblem& x, const MxProblem& y) { return x.k > y.k; });   // the longest begin
+  std::sort(ps.pr, ps.pr + ps.n, [](const MxProblem& x, const MxProblem& y) { return x.units > y.units; });   // the longest begin
   const int64_t large = count_tiles(ps, 256, 256), small = count_tiles(ps, 128, 128);
   int64_t units = 0;   // of all small tiles along k
-  for (int i = 0; i < ps.n; ++i) units += ((i + 1 < ps.n ? ps.pr[i + 1].first_tile : small) - ps.pr[i].first_tile) * mx_k_units(ps.pr[i].k);
+  for (int i = 0; i < ps.n; ++i) units += static_cast<int64_t>(ps.first_tile[i + 1] - ps.first_tile[i]) * ps.pr[i].units;
   const int64_t ks = (units + small - 1) / small;
   if (large_tiles_ns(large, ks) < small_tiles_ns(small, ks)) {
     launch_large_tiles<float, false>(ps, st);
@@ -670,7 +692,7 @@ hipError_t launch_tiles(MxProblems& ps, hipStream_t st) {
     launch_large_tiles<float, true>(ps, st);
     launch_large_tiles<__bf16, true>(ps, st);
   } else {
-    k_mx_product<4, void, false><<<tile_grid(ps, small, 2 * N_CU), THREADS, 0, st>>>(ps);
+    k_mx_product<4, void, false><<<tile_grid(ps, 2 * N_CU), THREADS, 0, st>>>(ps);
   }
   return hipGetLastError();
 }
@@ -734,6 +756,11 @@ hipError_t launch_kind(int kind, MxProblems& ps, hipStream_t st) {
 }
 
 }  // namespace
+
+hipError_t launch_mx_join(const MxProblem& p, const float* sums, int parts, hipStream_t st) {
+  k_mx_join<<<dim3(static_cast<unsigned>(std::min<int64_t>((p.m * p.n + THREADS - 1) / THREADS, 16 * N_CU))), THREADS, 0, st>>>(p, sums, parts);
+  return hipGetLastError();
+}
 
 hipError_t launch_mx_product(const MxProblems& ps, hipStream_t st) {
   int kind[MX_MAX_PROBLEMS];

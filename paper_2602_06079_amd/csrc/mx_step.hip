@@ -92,11 +92,19 @@ int check_product_group(const canz_mx_product_group& g, int idx, bool need_ptrs)
 // whether A is rounded by a launch of its own, into an image in the workspace
 bool mx_rounded_before(const canz_mx_product_group& g) { return !mx_idle(g) && g.k > 0 && g.a_dtype != CANZ_DT_MX && !mx_rounds_on_the_way(g.m, g.n, g.k); }
 
-// room for these images
+// bytes of the sums of the parts that k is cut into
+size_t mx_part_bytes(int64_t m, int64_t n, int64_t k) {
+  const int parts = mx_parts(m, n, k);
+  return parts > 1 ? (static_cast<size_t>(parts) * m * n * sizeof(float) + ALIGN - 1) / ALIGN * ALIGN : 0;
+}
+
+// room for these images, and for these sums
 size_t product_workspace(const canz_mx_product_group* g, int32_t n_groups) {
   size_t need = 0;
-  for (int i = 0; i < n_groups; ++i)
-    if (mx_rounded_before(g[i])) need += static_cast<size_t>(g[i].n_prods) * mx_image_bytes(g[i].m, g[i].k);
+  for (int i = 0; i < n_groups; ++i) {
+    if (mx_idle(g[i])) continue;
+    need += static_cast<size_t>(g[i].n_prods) * ((mx_rounded_before(g[i]) ? mx_image_bytes(g[i].m, g[i].k) : 0) + mx_part_bytes(g[i].m, g[i].n, g[i].k));
+  }
   return std::max(need, ALIGN);
 }
 
@@ -201,20 +209,29 @@ extern "C" int canz_mx_product(const canz_mx_product_group* g, int32_t n_groups,
   }
   if (int rc = round()) return rc;
 
+  uint8_t* sums = images + at;
+  at = 0;
   MxProblems ps;
   ps.n = 0;
+  struct Join {
+    MxProblem p;
+    const float* sums;
+    int parts;
+  } joins[MX_MAX_PROBLEMS];
+  int n_joins = 0;
   auto flush = [&]() -> int {
-    const hipError_t err = launch_mx_product(ps, st);
-    ps.n = 0;
+    hipError_t err = launch_mx_product(ps, st);
+    for (int i = 0; i < n_joins && err == hipSuccess; ++i) err = launch_mx_join(joins[i].p, joins[i].sums, joins[i].parts, st);
+    ps.n = n_joins = 0;
     return err == hipSuccess ? CANZ_OK : fail(CANZ_EHIP, "microscaled product: %s", hipGetErrorString(err));
   };
-  at = 0;
   for (int i = 0; i < n_groups; ++i) {
     const canz_mx_product_group& gi = g[i];
     if (mx_idle(gi)) continue;
     const bool before = mx_rounded_before(gi);
+    const int parts = mx_parts(gi.m, gi.n, gi.k), units = static_cast<int>(mx_k_units(gi.k));
     for (int x = 0; x < gi.n_prods; ++x) {
-      MxProblem& p = ps.pr[ps.n++];
+      MxProblem p{};
       p.a = before ? images + at : static_cast<const uint8_t*>(gi.k > 0 ? gi.a[x] : nullptr);
       if (before) at += static_cast<size_t>(mx_image_bytes(gi.m, gi.k));
       p.a_dtype = before ? CANZ_DT_MX : gi.a_dtype, p.a_ceil = gi.a_scale_mode == CANZ_MX_SCALE_CEIL, p.lda = gi.lda;
@@ -222,8 +239,22 @@ extern "C" int canz_mx_product(const canz_mx_product_group* g, int32_t n_groups,
       p.c = gi.c[x];
       p.m = gi.m, p.n = gi.n, p.k = gi.k, p.ldc = gi.ldc;
       p.alpha = gi.alpha, p.beta = gi.beta, p.out_dtype = gi.out_dtype;
-      if (ps.n == MX_MAX_PROBLEMS)
+      p.units = units;
+      if (ps.n + parts > MX_MAX_PROBLEMS)
         if (int rc = flush()) return rc;
+      if (parts == 1) {
+        ps.pr[ps.n++] = p;
+        continue;
+      }
+      joins[n_joins++] = Join{p, reinterpret_cast<const float*>(sums), parts};
+      for (int q = 0; q < parts; ++q) {   // whole rounds of the kernel's ring, but for the last part; at least 5 units (mx_parts)
+        MxProblem& part = ps.pr[ps.n++] = p;
+        part.first_unit = q * units / parts / 4 * 4;
+        part.units = (q + 1 < parts ? (q + 1) * units / parts / 4 * 4 : units) - part.first_unit;
+        part.c = sums + static_cast<size_t>(q) * p.m * p.n * sizeof(float);
+        part.ldc = p.n, part.alpha = 1.f, part.beta = 0.f, part.out_dtype = CANZ_DT_F32;
+      }
+      sums += mx_part_bytes(gi.m, gi.n, gi.k);
     }
   }
   return ps.n > 0 ? flush() : CANZ_OK;

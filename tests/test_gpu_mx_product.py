@@ -76,7 +76,31 @@ def test_exact_sums(canz, m, n, k):
         assert np.isnan(got[m:]).all() and np.isnan(got[:, n:]).all()
 
 
-@pytest.mark.parametrize("m,n,k", [(1, 300, 5000), (7, 129, 20000), (40, 70, 3000), (300, 260, 4100)])
+@pytest.mark.parametrize("m,n,k", [(65, 100, 16000), (128, 128, 8192), (200, 300, 9001), (513, 400, 7000)])
+def test_long_k_in_parts(canz, m, n, k):
+    """Few tiles and a long k: k is cut into parts whose sums are joined.  Products that are multiples of 1/4, so that all sums are exact; alone, accumulating
+    on an earlier result, and in one call with products that are not cut."""
+    import torch
+    assert 36 * k * 4 < 2 ** 24
+    rng = np.random.default_rng(k)
+    a, b, b2 = operand(rng, m, k), operand(rng, n, k), operand(rng, 2000, k)
+    want = MX.product(MX.values(*a), MX.values(*b))
+    da, db, db2 = device(a), device(b), device(b2)
+    c = torch.full((m, n + 3), float("nan"), device="cuda")
+    groups = [canz.MxProduct(m=m, n=n, k=k, a=[da], b=[db], c=[c], ldc=n + 3, out_dtype=W.DT_F32)]
+    assert canz.canz_mx_product_workspace_bytes(groups) > 256          # it is cut
+    run(canz, groups)
+    assert np.array_equal(c.double().cpu().numpy()[:, :n], want) and torch.isnan(c[:, n:]).all()
+    old = torch.from_numpy(rng.integers(-50, 50, (m, n)).astype(np.float32)).to(torch.bfloat16).cuda()
+    h, e = old.clone(), torch.empty(m, 2000, device="cuda")
+    run(canz, [canz.MxProduct(m=m, n=n, k=k, a=[da, da], b=[db, db], c=[h, old], alpha=0.5, beta=2.0),
+               canz.MxProduct(m=m, n=2000, k=k, a=[da], b=[db2], c=[e], out_dtype=W.DT_F32)] +
+              [canz.MxProduct(m=m, n=n, k=k, a=[da], b=[db], c=[torch.empty(m, n, device="cuda")], out_dtype=W.DT_F32) for _ in range(9)])
+    assert torch.equal(h, old)
+    assert np.array_equal(e.double().cpu().numpy(), MX.product(MX.values(*a), MX.values(*b2)))
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 300, 5000), (7, 129, 20000), (40, 70, 3000), (300, 260, 4100), (130, 260, 20000)])
 def test_wide_scales(canz, m, n, k):
     import torch
     rng = np.random.default_rng(k)
