@@ -268,6 +268,8 @@ extern "C" int canz_muon_step_images(const canz_group* g, int32_t n_groups, cons
   if (hp->out_mode != CANZ_OUT_PARAM) return fail(CANZ_EUNSUPPORTED, "images are taken of updated parameters: out_mode must be CANZ_OUT_PARAM");
   if (int rc = check_scale_mode(scale_mode)) return rc;
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  const StreamDevice on(st);
+  if (on.error() != hipSuccess) return fail(CANZ_EHIP, "stream: %s", hipGetErrorString(on.error()));
   // everything is checked before the step is enqueued; the second time round the images are
   for (int pass = 0; pass < 2; ++pass) {
     for (int i = 0; i < n_groups; ++i) {

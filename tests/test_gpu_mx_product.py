@@ -408,3 +408,58 @@ def test_large_offsets(canz):
     run(canz, [canz.MxProduct(m=m, n=n, k=k, a=[ix], b=[iy], c=[c])])
     assert not c[:-256].any() and not c[:, :-256].any()
     assert np.array_equal(c[-256:, -256:].double().cpu().numpy(), to_bf16(MX.product(MX.values(*a), MX.values(*b))))
+
+
+def test_longest_k_and_most_rows(canz):
+    """The documented limit of an extent, with ones: sums of 4194240 < 2^24 are exact."""
+    import torch
+    top = 4194240
+    ones = lambda r, c: torch.ones(r, c, dtype=torch.bfloat16, device="cuda")
+    image = lambda r, c: torch.empty(canz.canz_mx_image_bytes(r, c), dtype=torch.uint8, device="cuda")
+    a, b = image(65, top), image(40, top)
+    x, y = ones(65, top), ones(40, top)
+    x[:, -1] = 2.0
+    canz.canz_mx_quantize([canz.MxGroup(rows=65, cols=top, mat=[x], by_row=[a], dtype=W.DT_BF16), canz.MxGroup(rows=40, cols=top, mat=[y], by_row=[b], dtype=W.DT_BF16)],
+                          0, stream())
+    c, c1 = torch.empty(65, 40, device="cuda"), torch.empty(1, 40, device="cuda")
+    run(canz, [canz.MxProduct(m=65, n=40, k=top, a=[a], b=[b], c=[c], out_dtype=W.DT_F32),
+               canz.MxProduct(m=1, n=40, k=top, a=[x], b=[b], c=[c1], a_dtype=W.DT_BF16, out_dtype=W.DT_F32)])
+    assert (c == top + 1).all() and (c1 == top + 1).all()
+    del x, y, a, b
+    w, v = image(top, 33), torch.ones(top, 33, dtype=torch.bfloat16, device="cuda")
+    v[-1] = 4.0
+    t = image(33, top)
+    canz.canz_mx_quantize([canz.MxGroup(rows=top, cols=33, mat=[v], by_row=[w], by_col=[t], dtype=W.DT_BF16)], 0, stream())
+    row = torch.full((1, top), float("nan"), device="cuda")
+    run(canz, [canz.MxProduct(m=1, n=top, k=33, a=[ones(1, 33)], b=[w], c=[row], a_dtype=W.DT_BF16, out_dtype=W.DT_F32)])
+    assert (row[0, :-1] == 33).all() and row[0, -1] == 132
+    gram = torch.empty(33, 33, device="cuda")
+    run(canz, [canz.MxProduct(m=33, n=33, k=top, a=[t], b=[t], c=[gram], out_dtype=W.DT_F32)])
+    assert (gram == top - 1 + 16).all()
+
+
+def test_calls_at_once_on_two_streams(canz):
+    """Products that are split, that are not, and of few rows, on two streams at a time with workspaces of their own."""
+    import torch
+    rng = np.random.default_rng(17)
+    jobs = []
+    for s in range(2):
+        groups = []
+        for m, n, k in ((100, 200, 9000), (300, 700, 1000), (9, 500, 3000)):
+            x = torch.from_numpy(rng.standard_normal((m, k)).astype(np.float32)).cuda()
+            groups.append(canz.MxProduct(m=m, n=n, k=k, a=[x], b=[device(operand(rng, n, k, 2))], c=[torch.empty(m, n, device="cuda")], a_dtype=W.DT_F32,
+                                         out_dtype=W.DT_F32))
+        run(canz, groups)
+        jobs.append((groups, [g.c[0].clone() for g in groups], workspace(canz, groups), torch.cuda.Stream()))
+    for rep in range(5):
+        for groups, _, _, _ in jobs:
+            for g in groups:
+                g.c[0].fill_(float("nan"))
+        torch.cuda.synchronize()
+        for _ in range(3):
+            for groups, _, ws, st in jobs:
+                canz.canz_mx_product(groups, ws, ws.numel(), st.cuda_stream)
+        torch.cuda.synchronize()
+        for groups, want, _, _ in jobs:
+            for g, w in zip(groups, want):
+                assert torch.equal(g.c[0], w)
