@@ -478,7 +478,8 @@ int canz_muon_step_static(const canz_group* g, int32_t n_groups, const canz_muon
  * 4194240 each and padded matrices at most 2^37 elements; an extent may be 0, and then nothing is read or written (k = 0 in a product:
  * C <- beta C) and the pointers of that matrix may be NULL.  Tables are host arrays of device pointers, read during the call.
  * The calls issue kernel launches only (no allocation, copy, memset or synchronisation), on the device hip_stream
- * belongs to (NULL: the current one), and may be recorded into a HIP graph.  Results do not depend on what else is in the call.
+ * belongs to (NULL: the current one), and may be recorded into a HIP graph.  What a call writes must not overlap any other buffer of the call; what
+ * it only reads may be given any number of times.  Results do not depend on what else is in the call.
  */
 enum { CANZ_MX_SCALE_FLOOR = 0, CANZ_MX_SCALE_CEIL = 1 };
 
@@ -515,8 +516,8 @@ int canz_mx_dequantize(const canz_mx_group* g, int32_t n_groups, void* hip_strea
 /*
  * Products of one shape: C = alpha A B^T + beta C with A (m x k) and B (n x k).  B is an image.  A is an image (CANZ_DT_MX) or a
  * row-major matrix that the call rounds as canz_mx_quantize does, to the nearest values with a_scale_mode; the result is the same.
- * Products of two elements are exact, sums over k are in fp32 (their order depends on m, n and k alone), and an element is rounded once to the type of
- * C.  C is not read where beta is 0.  C must not overlap another buffer of the call.
+ * Products of two elements are exact within the normal range of fp32, sums over k are in fp32 (their order depends on m, n and k alone), and an
+ * element is rounded once to the type of C.  C is not read where beta is 0.
  */
 typedef struct {
   int64_t m, n, k;
@@ -540,7 +541,8 @@ int canz_mx_product_workspace_bytes(const canz_mx_product_group* g, int32_t n_gr
  * them), and all products of a call may run at once.
  *   workspace       device, 256-byte aligned, caller-owned scratch that need not be initialised; not to be shared by calls that may
  *                   run at the same time (two streams, two graphs)
- * Errors: CANZ_EINVAL, CANZ_ESHAPE, CANZ_EUNSUPPORTED, CANZ_EHIP as canz_mx_quantize; CANZ_EWORKSPACE.
+ * Errors: CANZ_EINVAL, CANZ_ESHAPE, CANZ_EUNSUPPORTED, CANZ_EHIP as canz_mx_quantize, and CANZ_ESHAPE if the workspace had more than
+ * 2^64 bytes; CANZ_EWORKSPACE.
  */
 int canz_mx_product(const canz_mx_product_group* g, int32_t n_groups, void* workspace, size_t workspace_bytes,
                     void* hip_stream);

@@ -517,7 +517,7 @@ assert _MX_GROUP.size == C.sizeof(_MxGroup) and _MX_PRODUCT.size == C.sizeof(_Mx
 
 def _table(seq, keep, n):
     """Address of the host table of n device addresses; empty: a null table."""
-    if not seq:
+    if seq is None or len(seq) == 0:
         return 0
     if len(seq) != n:
         raise ValueError("a table of %d buffers where the group has %d" % (len(seq), n))

@@ -38,10 +38,10 @@ constexpr size_t ALIGN = 256;
 template <typename F>
 int for_each_launch(const canz_mx_group& g, int scale_mode, bool noise, F&& fn) {
   if (g.rows == 0 || g.cols == 0) return CANZ_OK;
-  for (int first = 0; first < g.n_mats; first += MX_MAX_MATS) {
+  for (int64_t first = 0; first < g.n_mats; first += MX_MAX_MATS) {
     MxMats m{};
     m.most_rows = g.rows, m.cols = g.cols, m.ld = g.ld;
-    m.n = std::min(MX_MAX_MATS, g.n_mats - first);
+    m.n = static_cast<int>(std::min<int64_t>(MX_MAX_MATS, g.n_mats - first));
     m.dtype = g.dtype, m.scale_mode = scale_mode;
     for (int i = 0; i < m.n; ++i) {
       m.rows[i] = static_cast<int>(g.rows);
@@ -99,13 +99,17 @@ size_t mx_part_bytes(int64_t m, int64_t n, int64_t k) {
 }
 
 // room for these images, and for these sums
-size_t product_workspace(const canz_mx_product_group* g, int32_t n_groups) {
+int product_workspace(const canz_mx_product_group* g, int32_t n_groups, size_t* bytes_out) {
   size_t need = 0;
   for (int i = 0; i < n_groups; ++i) {
     if (mx_idle(g[i])) continue;
-    need += static_cast<size_t>(g[i].n_prods) * ((mx_rounded_before(g[i]) ? mx_image_bytes(g[i].m, g[i].k) : 0) + mx_part_bytes(g[i].m, g[i].n, g[i].k));
+    const size_t each = (mx_rounded_before(g[i]) ? mx_image_bytes(g[i].m, g[i].k) : 0) + mx_part_bytes(g[i].m, g[i].n, g[i].k);
+    size_t group = 0;
+    if (__builtin_mul_overflow(each, static_cast<size_t>(g[i].n_prods), &group) || __builtin_add_overflow(need, group, &need))
+      return fail(CANZ_ESHAPE, "group %d: the workspace would have more bytes than 64 bits count", i);
   }
-  return std::max(need, ALIGN);
+  *bytes_out = std::max(need, ALIGN);
+  return CANZ_OK;
 }
 
 }  // namespace
@@ -160,8 +164,7 @@ extern "C" int canz_mx_product_workspace_bytes(const canz_mx_product_group* g, i
   if (n_groups < 0 || (n_groups > 0 && !g)) return fail(CANZ_EINVAL, "bad group array");
   for (int i = 0; i < n_groups; ++i)
     if (int rc = check_product_group(g[i], i, false)) return rc;
-  *bytes_out = product_workspace(g, n_groups);
-  return CANZ_OK;
+  return product_workspace(g, n_groups, bytes_out);
 }
 
 extern "C" int canz_mx_product(const canz_mx_product_group* g, int32_t n_groups, void* workspace, size_t workspace_bytes,
@@ -176,7 +179,8 @@ extern "C" int canz_mx_product(const canz_mx_product_group* g, int32_t n_groups,
   if (!any) return CANZ_OK;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & (ALIGN - 1)))
     return fail(CANZ_EWORKSPACE, "workspace null or not 256-byte aligned");
-  const size_t need = product_workspace(g, n_groups);
+  size_t need = 0;
+  if (int rc = product_workspace(g, n_groups, &need)) return rc;
   if (workspace_bytes < need) return fail(CANZ_EWORKSPACE, "workspace too small: %zu bytes given, %zu needed", workspace_bytes, need);
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
   const StreamDevice on(st);

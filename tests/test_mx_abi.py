@@ -122,6 +122,21 @@ def test_product_refusals_and_workspace(canz):
     canz.canz_mx_product([P(m=0, n=5, k=5, n_prods=2), P(m=5, n=0, k=5, n_prods=2), P(m=5, n=5, k=5, n_prods=0)], 0, 0, 0)
 
 
+def test_workspace_past_64_bits_is_refused(canz):
+    P = canz.MxProduct
+    many = dict(m=1 << 18, n=128, k=1 << 19, n_prods=(1 << 31) - 1, a_dtype=canz.DT_BF16)   # 7.3e10 bytes of image each
+    assert canz.canz_mx_product_workspace_bytes([P(**{**many, "n_prods": 1000})]) >= 1000 * canz.canz_mx_image_bytes(1 << 18, 1 << 19)
+    assert _code(canz, canz.canz_mx_product_workspace_bytes, [P(**many)]) == canz.ESHAPE
+    assert _code(canz, canz.canz_mx_product_workspace_bytes, [P(**{**many, "n_prods": 1 << 27})] * 3) == canz.ESHAPE   # their sum
+
+
+def test_tables_may_be_any_sequence(canz):
+    np = pytest.importorskip("numpy")
+    for kind in (tuple, np.array):
+        assert _code(canz, canz.canz_mx_quantize, [canz.MxGroup(rows=64, cols=128, mat=kind([4096, 8192]), by_row=kind([8192, 8200]))], 0, 0) == canz.EINVAL
+        assert "by_row[1]" in canz.canz_last_error()
+
+
 def test_step_images_refusals(canz):
     ok = dict(rows=256, cols=512, grad=[4096], mom=[8192], out=[12288])
 
