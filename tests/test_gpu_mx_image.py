@@ -221,3 +221,22 @@ def test_large_matrix_offsets(canz):
         else:
             want = MX.values(*MX.quantize(held, 0))
         assert np.array_equal(got, want)
+
+
+@pytest.mark.parametrize("shift", [1, 2, 3])
+def test_noise_anywhere(canz, shift):
+    """Noise bytes at addresses of any alignment, rows of odd length, and the largest and smallest noise there is."""
+    import torch
+    rows, cols = 131, 77
+    x = hard_values(rows, cols, 40 + shift)
+    buf, held = device_matrix(x, W.DT_F32, cols)
+    for u in (np.random.default_rng(shift).integers(0, 256, (rows, cols)).astype(np.uint8), np.zeros((rows, cols), np.uint8), np.full((rows, cols), 255, np.uint8)):
+        around = torch.full((rows * cols + 8,), 200, dtype=torch.uint8, device="cuda")
+        noise = around[shift:shift + rows * cols]
+        noise.copy_(torch.from_numpy(u.ravel()))
+        assert noise.data_ptr() % 4 == shift
+        a, b = Image(canz, rows, cols), Image(canz, cols, rows)
+        canz.canz_mx_quantize([canz.MxGroup(rows=rows, cols=cols, mat=[buf], by_row=[a], by_col=[b], noise=[noise])], MX.FLOOR, stream())
+        torch.cuda.synchronize()
+        a.check(held, MX.FLOOR, u)
+        b.check(held.T, MX.FLOOR, u.T)

@@ -463,3 +463,48 @@ def test_calls_at_once_on_two_streams(canz):
         for groups, want, _, _ in jobs:
             for g, w in zip(groups, want):
                 assert torch.equal(g.c[0], w)
+
+
+def test_every_kind_in_one_call(canz):
+    """Products of every size class, type and beta in one call, operands shared among them, in a workspace of exactly the bytes asked for between
+    guards: each has the bits it has alone, and nothing else is written."""
+    import torch
+    rng = np.random.default_rng(23)
+    kinds = [(1, 40, 500), (9, 40, 500), (16, 4100, 96), (17, 40, 500), (33, 40, 500), (64, 300, 260), (65, 300, 260), (300, 300, 260), (100, 200, 9000),
+             (7, 33, 0), (0, 40, 500), (70, 40, 8300), (600, 500, 130)]
+    b = {(n, k): device(operand(rng, n, k, 2)) for _, n, k in kinds if k}
+    groups, outs = [], []
+    for i, (m, n, k) in enumerate(kinds * 3):
+        a_dtype = (W.DT_BF16, W.DT_F32, canz.DT_MX)[i // len(kinds)]
+        out_dtype, beta = (W.DT_F32, W.DT_BF16)[i % 2], 0.5 * (i % 3)
+        dt = torch.float32 if out_dtype == W.DT_F32 else torch.bfloat16
+        lda, ldc = k + i % 4, n + i % 5
+        if k == 0:
+            a = 0
+        elif a_dtype == canz.DT_MX:
+            a = device(operand(rng, max(m, 1), k, 2))
+        else:
+            a = torch.from_numpy(rng.standard_normal((max(m, 1), lda)).astype(np.float32)).to(torch.bfloat16 if a_dtype == W.DT_BF16 else torch.float32).cuda()
+        c = torch.from_numpy(rng.standard_normal((m + 1, ldc)).astype(np.float32)).to(dt).cuda()
+        groups.append(canz.MxProduct(m=m, n=n, k=k, a=[a], b=[b.get((n, k), 0)], c=[c], lda=lda, ldc=ldc, alpha=1.5, beta=beta, a_dtype=a_dtype,
+                                     out_dtype=out_dtype))
+        outs.append(c)
+    before = [c.clone() for c in outs]
+
+    def call(gs):
+        need = canz.canz_mx_product_workspace_bytes(gs)
+        ws = torch.full((need + 512,), 0xFF, dtype=torch.uint8, device="cuda")
+        canz.canz_mx_product(gs, ws.data_ptr() + 256, need, stream())
+        torch.cuda.synchronize()
+        assert (ws[:256] == 0xFF).all() and (ws[256 + need:] == 0xFF).all()
+    call(groups)
+    together = [c.clone() for c in outs]
+    for c, x in zip(outs, before):
+        c.copy_(x)
+    for g in groups:
+        call([g])
+    for c, t, x, g in zip(outs, together, before, groups):
+        assert torch.equal(c, t)
+        assert torch.equal(c[g.m:], x[g.m:]) and torch.equal(c[:, g.n:], x[:, g.n:])
+        if g.m and (g.k or g.beta != 1.0):
+            assert not torch.equal(c[:g.m, :g.n], x[:g.m, :g.n])
