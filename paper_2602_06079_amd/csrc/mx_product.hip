@@ -398,7 +398,7 @@ struct Stage {
   static constexpr int code_loads = W, scale_loads = W / 4, loads = code_loads + scale_loads;   // of one wavefront
 };
 
-// What a block has to do and has to load next: the tiles slot, slot + grid, ...
+// What a block has to do and has to load next: of the launch's tiles those numbered blockIdx.x, blockIdx.x + gridDim.x, ... (tile_at)
 struct Tile {
   int problem;   // -1: none
   int m0, n0;    // in units of 16 rows
@@ -661,8 +661,9 @@ constexpr int N_CU = 256;
 
 // ns that a launch takes by the tiles it has: 256 x 256 in rounds of one to a CU, 128 x 128 in rounds of two, or less than one at the end.  A k unit
 // takes 780 ns of a round of large tiles and 460 of one of small ones (a quarter of the work, twice as often), 210 with one small tile to a CU; beginning
-// and end of a tile 6000 and 2600.  us, 256 x 256 and 128 x 128: 8192^3 229, 256; 4096^3 36, 39; 8192 x 12288 x 4096 195, 212; 4096 x 25600 x 5120 269, 269;
-// 6000 x 6000 x 2000 61, 50; 4096 x 4096 x 1024 17.5, 16.4; 2048 x 4096 x 8192 51, 35; 4096 x 2048 x 1024 16.2, 10.8; 1024^3 13.3, 6.1.
+// and end of a tile 6000 and 2600.  us for bf16 results, 256 x 256 and 128 x 128: 8192^3 223, 252; 4096^3 35, 36; 8192 x 12288 x 4096 189, 213; 4096 x
+// 25600 x 5120 246, 256; 6000 x 6000 x 2000 52, 42; 5000 x 4000 x 1000 28, 19; 4096 x 4096 x 1024 18.1, 16.8; 3000^3 25, 21; 2048 x 4096 x 8192 49, 35;
+// 4096 x 2048 x 1024 15.7, 10.8; 1024^3 13.6, 6.3.
 int64_t large_tiles_ns(int64_t tiles, int64_t ks) { return (tiles + N_CU - 1) / N_CU * (780 * ks + 6000); }
 int64_t small_tiles_ns(int64_t tiles, int64_t ks) {
   const int64_t rest = tiles % (2 * N_CU);
