@@ -34,6 +34,23 @@ __device__ __forceinline__ unsigned noisy_code(float v, unsigned byte, unsigned 
   constexpr unsigned SIGN = 1u << 11;
   return sum | (__builtin_bit_cast(unsigned, v) >> 20 & SIGN);   // LIMIT and what the sums reach leave bit 11 free
 }
+// The same for two bf16 elements at a time, whose eight digits fp16 holds: half the instructions.  `less`: their blocks' (byte - 16) << 7, byte >= 16; u: noise
+// in the low bytes of the halves.  A difference of exponents makes 2 a in fp16 of |v| (what is below 2^-14 comes out as something below 2^-14 and is
+// rounded to 0 like it).  a + 2^(e + 1) is rounded to a multiple of 2^(e - 9) = s / 256, and the bits of the sum count these multiples; 512 e more and bits 8 and up
+// are the code.  Returned as by noisy_code, in either half.
+constexpr unsigned MX_PAIRS_FROM = 16;   // the smallest scale byte
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ unsigned noisy_pair(unsigned v, u16x2 less, unsigned u) {
+  const u16x2 twice = __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, v & 0x7FFF7FFFu), less) << 3;
+  constexpr unsigned short TWO = 0x4000, LIMIT = 0x7FF;
+  const unsigned top = __builtin_bit_cast(unsigned, __builtin_elementwise_max(twice, u16x2{TWO, TWO})) & 0x7C007C00u;   // 2^(e + 1): (e + 16) << 10
+  const f16x2 sum = __builtin_elementwise_fma(__builtin_bit_cast(f16x2, twice), f16x2{0.5f, 0.5f}, __builtin_bit_cast(f16x2, top));
+  const unsigned count = __builtin_bit_cast(unsigned, sum) + u - (top >> 1) - 0x20002000u;   // 0 .. 2303 in either half, so nothing is borrowed
+  const unsigned code = __builtin_bit_cast(unsigned, __builtin_elementwise_min(__builtin_bit_cast(u16x2, count), u16x2{LIMIT, LIMIT}));
+  return code | (v >> 4 & 0x08000800u);
+}
+
 // eight codes of one block, element 0 in the lowest bits; u: noise bytes
 template <bool NOISE>
 __device__ __forceinline__ unsigned eight_codes(const float (&v)[8], unsigned byte, const unsigned (&u)[8]) {
@@ -58,6 +75,14 @@ __device__ __forceinline__ unsigned eight_codes(const float (&v)[8], unsigned by
   return byte == MX_SCALE_NAN ? 0u : r;
 }
 
+// Codes of four words of noisy_pair as bytes: those of the low halves, those of the high ones
+__device__ __forceinline__ uint2 by_halves(unsigned p, unsigned q, unsigned r, unsigned s) {
+  constexpr unsigned BYTES_1_3 = 0x07030501u, LOW = 0x05040100u, HIGH = 0x07060302u;
+  const unsigned pq = __builtin_amdgcn_perm(q, p, BYTES_1_3), rs = __builtin_amdgcn_perm(s, r, BYTES_1_3);
+  return {__builtin_amdgcn_perm(rs, pq, LOW), __builtin_amdgcn_perm(rs, pq, HIGH)};
+}
+constexpr unsigned NOISE_LOW = 0x0C010C00u, NOISE_HIGH = 0x0C030C02u;   // two of four noise bytes, a half each
+
 // the largest of the four lanes that hold a block
 __device__ __forceinline__ unsigned largest_of_four(unsigned v) {
   constexpr int SWAP_1 = 0xB1, SWAP_2 = 0x4E;   // quad permutes [1, 0, 3, 2] and [2, 3, 0, 1]
@@ -80,7 +105,6 @@ struct PairMax<float> {
 };
 template <>
 struct PairMax<__bf16> {
-  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
   u16x2 top = {0, 0};
   __device__ __forceinline__ void take(mx_bf16x2 x) { top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, __builtin_bit_cast(unsigned, x) & 0x7FFF7FFFu)); }
   __device__ __forceinline__ unsigned of(int q) const { return static_cast<unsigned>(top[q]) << 16; }
@@ -143,6 +167,7 @@ __device__ __forceinline__ void store8(E* p, int64_t left, const float (&v)[8]) 
 constexpr int ROWS = 128, COLS = 64;
 template <typename E, bool ROW, bool COL, bool NOISE>
 __global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {
+  constexpr bool PAIRS = NOISE && sizeof(E) == 2;   // two elements at a time where their scale allows it
   __shared__ E tile[COL ? ROWS * COLS : 1];
   __shared__ uint8_t tile_noise[COL && NOISE ? ROWS * COLS : 1];
   __shared__ unsigned row_scales[2][2][16], col_scales[4][16];   // 64 rows, block, slot; block, slot: dwords of the units' order
@@ -174,10 +199,22 @@ __global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {
 #pragma unroll
       for (int e = 0; e < 8; e += 2) top.take({static_cast<E>(v[e]), static_cast<E>(v[e + 1])});
       const unsigned byte = mx_scale_byte(largest_of_four(max(top.of(0), top.of(1))), ceil);
-      unsigned u[8];
+      unsigned codes;
+      if (PAIRS && byte >= MX_PAIRS_FROM) {
+        const unsigned short less = static_cast<unsigned short>((byte - MX_PAIRS_FROM) << 7);
+        unsigned p[4];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) u[e] = (e < 4 ? noise8.x : noise8.y) >> (8 * (e & 3)) & 255u;
-      const unsigned codes = eight_codes<NOISE>(v, byte, u);
+        for (int e = 0; e < 4; ++e)
+          p[e] = noisy_pair(__builtin_bit_cast(unsigned, mx_bf16x2{static_cast<__bf16>(v[2 * e]), static_cast<__bf16>(v[2 * e + 1])}), u16x2{less, less},
+                            __builtin_amdgcn_perm(0u, e < 2 ? noise8.x : noise8.y, e & 1 ? NOISE_HIGH : NOISE_LOW));
+        const uint2 even_odd = by_halves(p[0], p[1], p[2], p[3]);
+        codes = byte == MX_SCALE_NAN ? 0u : even_odd.x | even_odd.y << 4;
+      } else {
+        unsigned u[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) u[e] = (e < 4 ? noise8.x : noise8.y) >> (8 * (e & 3)) & 255u;
+        codes = eight_codes<NOISE>(v, byte, u);
+      }
       const int kb = (t & 7) >> 2;
       const int64_t unit = mx_unit(r0 + row);
       if (unit < mx_row_tiles(rows))
@@ -192,33 +229,68 @@ __global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {
     typedef E pair __attribute__((ext_vector_type(2)));
     const int c = (t & 31) * 2, rb = t >> 5;
     if (rb < ROWS / MX_BLOCK && c0 < m.cols) {
-      float v[2][MX_BLOCK];
-      unsigned n[MX_BLOCK];   // the noise of both
+      pair x[MX_BLOCK];
       PairMax<E> top;
 #pragma unroll
       for (int e = 0; e < MX_BLOCK; ++e) {
-        const int at = (rb * MX_BLOCK + e) * COLS + c;
-        const pair x = *reinterpret_cast<const pair*>(tile + at);
-        n[e] = 0;
-        if constexpr (NOISE) n[e] = *reinterpret_cast<const unsigned short*>(tile_noise + at);
-        top.take(x);
-        v[0][e] = static_cast<float>(x[0]), v[1][e] = static_cast<float>(x[1]);
+        x[e] = *reinterpret_cast<const pair*>(tile + (rb * MX_BLOCK + e) * COLS + c);
+        top.take(x[e]);
+      }
+      auto noise_of = [&](int e) CANZ_INLINE {   // of both
+        unsigned n = 0;
+        if constexpr (NOISE) n = *reinterpret_cast<const unsigned short*>(tile_noise + (rb * MX_BLOCK + e) * COLS + c);
+        return n;
+      };
+      const unsigned byte[2] = {mx_scale_byte(top.of(0), ceil), mx_scale_byte(top.of(1), ceil)};
+      u32x4 codes[2] = {{0u, 0u, 0u, 0u}, {0u, 0u, 0u, 0u}};
+      if (PAIRS && min(byte[0], byte[1]) >= MX_PAIRS_FROM) {
+        const u16x2 less = {static_cast<unsigned short>((byte[0] - MX_PAIRS_FROM) << 7), static_cast<unsigned short>((byte[1] - MX_PAIRS_FROM) << 7)};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          unsigned p[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            unsigned both = 0;
+            if constexpr (sizeof(E) == 2) both = __builtin_bit_cast(unsigned, x[w * 8 + e]);
+            p[e] = noisy_pair(both, less, __builtin_amdgcn_perm(0u, noise_of(w * 8 + e), NOISE_LOW));
+          }
+          const uint2 even = by_halves(p[0], p[2], p[4], p[6]), odd = by_halves(p[1], p[3], p[5], p[7]);
+          codes[0][w] = byte[0] == MX_SCALE_NAN ? 0u : even.x | odd.x << 4;
+          codes[1][w] = byte[1] == MX_SCALE_NAN ? 0u : even.y | odd.y << 4;
+        }
+      } else if constexpr (PAIRS) {   // rare: a rolled loop over what LDS holds, so that it takes no registers
+#pragma unroll 1
+        for (int w = 0; w < 4; ++w) {
+          const u32x4 rest[2] = {codes[0], codes[1]};
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            float v[8];
+            unsigned u[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              v[e] = static_cast<float>(tile[(rb * MX_BLOCK + w * 8 + e) * COLS + c + q]);
+              u[e] = noise_of(w * 8 + e) >> (8 * q) & 255u;
+            }
+            codes[q] = u32x4{rest[q][1], rest[q][2], rest[q][3], eight_codes<NOISE>(v, byte[q], u)};   // the vector turns instead of being indexed
+          }
+        }
+      } else {
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            float v[8];
+            unsigned u[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(x[w * 8 + e][q]), u[e] = noise_of(w * 8 + e) >> (8 * q) & 255u;
+            codes[q][w] = eight_codes<NOISE>(v, byte[q], u);
+          }
       }
       const int64_t unit = mx_unit(c0 + c);
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
-        const unsigned byte = mx_scale_byte(top.of(q), ceil);
-        u32x4 codes;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          float part[8];
-          unsigned u[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) part[e] = v[q][w * 8 + e], u[e] = n[w * 8 + e] >> (8 * q) & 255u;
-          codes[w] = eight_codes<NOISE>(part, byte, u);
-        }
-        *reinterpret_cast<u32x4*>(m.by_col[which] + (unit * units_col + r0 / MX_UNIT_K) * MX_UNIT_BYTES + (rb * 16 + mx_slot(c + q)) * 16) = codes;
-        reinterpret_cast<uint8_t*>(&col_scales[rb][mx_slot(c + q)])[mx_unit(c) % 4] = static_cast<uint8_t>(byte);
+        *reinterpret_cast<u32x4*>(m.by_col[which] + (unit * units_col + r0 / MX_UNIT_K) * MX_UNIT_BYTES + (rb * 16 + mx_slot(c + q)) * 16) = codes[q];
+        reinterpret_cast<uint8_t*>(&col_scales[rb][mx_slot(c + q)])[mx_unit(c) % 4] = static_cast<uint8_t>(byte[q]);
       }
     }
     __syncthreads();

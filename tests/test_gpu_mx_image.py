@@ -240,3 +240,29 @@ def test_noise_anywhere(canz, shift):
         torch.cuda.synchronize()
         a.check(held, MX.FLOOR, u)
         b.check(held.T, MX.FLOOR, u.T)
+
+
+@pytest.mark.parametrize("dtype", [W.DT_F32, W.DT_BF16])
+def test_noise_at_every_scale(canz, dtype):
+    """Blocks of every magnitude from denormal to the largest, each with all digits of its type and elements far below the largest, next to blocks of
+    very different magnitudes, zeros and NaN."""
+    import torch
+    rng = np.random.default_rng(61)
+    rows = cols = 32 * 9
+    exps = rng.permutation(np.arange(81 * 4) % 277 - 149)
+    for rep in range(4):
+        x = rng.uniform(1.0, 2.0, (rows, cols)) * rng.choice([-1, 1], (rows, cols))
+        x *= np.exp2(-rng.integers(0, 13, (rows, cols)).astype(np.float64)) * (rng.random((rows, cols)) < 0.95)
+        block = exps[rep * 81:rep * 81 + 81].reshape(9, 9)
+        x = (x * np.exp2(np.repeat(np.repeat(block, 32, 0), 32, 1).astype(np.float64))).astype(np.float32)
+        x[5, 40] = np.nan
+        x[77, 200] = -np.inf
+        u = rng.integers(0, 256, (rows, cols)).astype(np.uint8)
+        buf, held = device_matrix(x, dtype, cols)
+        a, b = Image(canz, rows, cols), Image(canz, cols, rows)
+        for mode in (MX.FLOOR, MX.CEIL):
+            canz.canz_mx_quantize([canz.MxGroup(rows=rows, cols=cols, mat=[buf], by_row=[a], by_col=[b], noise=[torch.from_numpy(u).cuda()], dtype=dtype)],
+                                  mode, stream())
+            torch.cuda.synchronize()
+            a.check(held, mode, u)
+            b.check(held.T, mode, u.T)
