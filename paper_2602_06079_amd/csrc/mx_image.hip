@@ -112,27 +112,26 @@ struct PairMax<__bf16> {
 
 // eight consecutive elements of a row, those behind its end as zeros
 template <typename E>
-__device__ __forceinline__ void load8(const E* p, int64_t left, float (&v)[8]) {
-  if (left >= 8) {
-    if constexpr (sizeof(E) == 4) {
-      const f32x4_any a = *reinterpret_cast<const f32x4_any*>(p), b = *reinterpret_cast<const f32x4_any*>(p + 4);
+using Eight = E __attribute__((ext_vector_type(8)));
+template <typename E>
+__device__ __forceinline__ Eight<E> load8(const E* p) {
+  typedef E any __attribute__((ext_vector_type(8), aligned(sizeof(E))));
+  return *reinterpret_cast<const any*>(p);
+}
+template <typename E>
+__device__ __forceinline__ Eight<E> load8(const E* p, int64_t left) {
+  if (left >= 8) return load8(p);
+  Eight<E> v;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
-    } else {
-      const bf16x8_any a = *reinterpret_cast<const bf16x8_any*>(p);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = static_cast<float>(a[i]);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < left ? static_cast<float>(p[i]) : 0.f;
-  }
+  for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : static_cast<E>(0.f);
+  return v;
+}
+__device__ __forceinline__ uint2 load_noise8(const uint8_t* p) {
+  const u32x2_any w = *reinterpret_cast<const u32x2_any*>(p);
+  return uint2{w[0], w[1]};
 }
 __device__ __forceinline__ uint2 load_noise8(const uint8_t* p, int64_t left) {
-  if (left >= 8) {
-    const u32x2_any w = *reinterpret_cast<const u32x2_any*>(p);
-    return uint2{w[0], w[1]};
-  }
+  if (left >= 8) return load_noise8(p);
   uint2 r = {0, 0};
 #pragma unroll
   for (int i = 0; i < 8; ++i) (i < 4 ? r.x : r.y) |= i < left ? static_cast<unsigned>(p[i]) << (8 * (i & 3)) : 0u;
@@ -168,8 +167,8 @@ constexpr int ROWS = 128, COLS = 64;
 template <typename E, bool ROW, bool COL, bool NOISE>
 __global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {
   constexpr bool PAIRS = NOISE && sizeof(E) == 2;   // two elements at a time where their scale allows it
-  __shared__ E tile[COL ? ROWS * COLS : 1];
-  __shared__ uint8_t tile_noise[COL && NOISE ? ROWS * COLS : 1];
+  __shared__ __attribute__((aligned(32))) E tile[COL ? ROWS * COLS : 1];
+  __shared__ __attribute__((aligned(8))) uint8_t tile_noise[COL && NOISE ? ROWS * COLS : 1];
   __shared__ unsigned row_scales[2][2][16], col_scales[4][16];   // 64 rows, block, slot; block, slot: dwords of the units' order
   const int t = threadIdx.x, which = blockIdx.z;
   const int64_t r0 = static_cast<int64_t>(blockIdx.y) * ROWS, c0 = static_cast<int64_t>(blockIdx.x) * COLS;
@@ -181,17 +180,36 @@ __global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {
   const int kb0 = static_cast<int>(c0 / MX_BLOCK) & 3;                            // 0 or 2: the tile is one half of a k unit of by_row
 
   const int col = (t & 7) * 8;
+  constexpr int EACH = ROWS / 32;   // rows of a thread
+  Eight<E> x8[EACH];
+  uint2 n8[EACH];
+  const E* const from = src + (r0 + (t >> 3)) * m.ld + c0 + col;
+  const uint8_t* const noise_from = NOISE ? noise + (r0 + (t >> 3)) * m.cols + c0 + col : nullptr;
+  if (r0 + ROWS <= rows && c0 + COLS <= m.cols) {   // without a branch in between, so that all are on their way at once
 #pragma unroll
-  for (int i = 0; i < ROWS / 32; ++i) {
+    for (int i = 0; i < EACH; ++i) {
+      x8[i] = load8(from + i * 32 * m.ld);
+      n8[i] = {0, 0};
+      if constexpr (NOISE) n8[i] = load_noise8(noise_from + i * 32 * m.cols);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const int64_t left = r0 + i * 32 + (t >> 3) < rows ? m.cols - (c0 + col) : 0;
+      x8[i] = load8(from + i * 32 * m.ld, left);
+      n8[i] = {0, 0};
+      if constexpr (NOISE) n8[i] = load_noise8(noise_from + i * 32 * m.cols, left);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
     const int row = i * 32 + (t >> 3);
-    const int64_t left = r0 + row < rows ? m.cols - (c0 + col) : 0;
+    const uint2 noise8 = n8[i];
     float v[8];
-    load8(src + (r0 + row) * m.ld + c0 + col, left, v);
-    uint2 noise8 = {0, 0};
-    if constexpr (NOISE) noise8 = load_noise8(noise + (r0 + row) * m.cols + c0 + col, left);
-    if constexpr (COL) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) tile[row * COLS + col + e] = static_cast<E>(v[e]);
+    for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(x8[i][e]);
+    if constexpr (COL) {
+      *reinterpret_cast<Eight<E>*>(tile + row * COLS + col) = x8[i];
       if constexpr (NOISE) *reinterpret_cast<uint2*>(tile_noise + row * COLS + col) = noise8;
     }
     if constexpr (ROW) {
