@@ -158,6 +158,15 @@ __device__ __forceinline__ void store8(E* p, int64_t left, const float (&v)[8]) 
   }
 }
 
+// Tile (x, y) of a block: the RUN tiles after one another that a row of tiles has in it go to one XCD (dispatch goes round the XCDs block by block), since
+// neighbours share lines: all of noise, whose rows of a tile are 64 bytes, and all where rows do not begin on lines.
+constexpr int N_XCD = 8, RUN = 16;
+__device__ __forceinline__ uint2 tile_of_block() {
+  const unsigned n = gridDim.x * gridDim.y, id = blockIdx.x + gridDim.x * blockIdx.y, in = id % (N_XCD * RUN);
+  const unsigned tile = id - in + N_XCD * RUN <= n ? id - in + in % N_XCD * RUN + in / N_XCD : id;   // the last ones are left as they are
+  return {tile % gridDim.x, tile / gridDim.x};
+}
+
 // One block rounds a tile of 128 rows x 64 columns: first along its rows (8 lanes a row, 8 elements each, 4 lanes a block), keeping
 // the elements in LDS, then along its columns (a thread two blocks).  Scale bytes are collected in LDS and leave in pieces of 128 bytes and more.
 // Every element is read once and every image written once (the counters say 1.05 GB and 0.28 GB for two fp32 matrices of 25600 x 5120, both ways): 254 us, 5.2
@@ -171,7 +180,8 @@ __global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {
   __shared__ __attribute__((aligned(8))) uint8_t tile_noise[COL && NOISE ? ROWS * COLS : 1];
   __shared__ unsigned row_scales[2][2][16], col_scales[4][16];   // 64 rows, block, slot; block, slot: dwords of the units' order
   const int t = threadIdx.x, which = blockIdx.z;
-  const int64_t r0 = static_cast<int64_t>(blockIdx.y) * ROWS, c0 = static_cast<int64_t>(blockIdx.x) * COLS;
+  const uint2 at = tile_of_block();
+  const int64_t r0 = static_cast<int64_t>(at.y) * ROWS, c0 = static_cast<int64_t>(at.x) * COLS;
   const E* const src = static_cast<const E*>(m.mat[which]);
   const uint8_t* const noise = NOISE ? m.noise[which] : nullptr;
   const int ceil = m.scale_mode == CANZ_MX_SCALE_CEIL;
@@ -338,7 +348,8 @@ __global__ __launch_bounds__(THREADS) void k_mx_dequantize(MxMats m) {
   constexpr int LDT = TILE + 8 / sizeof(E);
   __shared__ E tile[COL ? TILE * LDT : 1];
   const int t = threadIdx.x, which = blockIdx.z;
-  const int64_t r0 = static_cast<int64_t>(blockIdx.y) * TILE, c0 = static_cast<int64_t>(blockIdx.x) * TILE;
+  const uint2 at = tile_of_block();
+  const int64_t r0 = static_cast<int64_t>(at.y) * TILE, c0 = static_cast<int64_t>(at.x) * TILE;
   E* const dst = static_cast<E*>(m.mat[which]);
   const int64_t rows = m.rows[which];
   if constexpr (COL) {
@@ -377,9 +388,9 @@ __global__ __launch_bounds__(THREADS) void k_mx_dequantize(MxMats m) {
     } else {
       const uint8_t* const img = m.by_row[which];
       const int64_t units = mx_k_units(m.cols), ks = c0 / MX_UNIT_K, unit = mx_unit(r0 + row);
-      const int at = ((t & 15) >> 2) * 16 + mx_slot(row);
-      const unsigned codes = *reinterpret_cast<const unsigned*>(img + (unit * units + ks) * MX_UNIT_BYTES + at * 16 + (t & 3) * 4);
-      const unsigned byte = img[mx_code_bytes(rows, m.cols) + (unit / 4 * units + ks) * MX_SCALE_BYTES + at * 4 + unit % 4];
+      const int slot = ((t & 15) >> 2) * 16 + mx_slot(row);
+      const unsigned codes = *reinterpret_cast<const unsigned*>(img + (unit * units + ks) * MX_UNIT_BYTES + slot * 16 + (t & 3) * 4);
+      const unsigned byte = img[mx_code_bytes(rows, m.cols) + (unit / 4 * units + ks) * MX_SCALE_BYTES + slot * 4 + unit % 4];
       eight_values(codes, byte, v);
     }
     store8(dst + (r0 + row) * m.ld + c0 + col, left, v);
