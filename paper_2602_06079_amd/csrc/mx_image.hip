@@ -34,12 +34,14 @@ __device__ __forceinline__ unsigned noisy_code(float v, unsigned byte, unsigned 
   constexpr unsigned SIGN = 1u << 11;
   return sum | (__builtin_bit_cast(unsigned, v) >> 20 & SIGN);   // LIMIT and what the sums reach leave bit 11 free
 }
-// The same for two bf16 elements at a time, whose eight digits fp16 holds: half the instructions.  `less`: their blocks' (byte - 16) << 7, byte >= 16; u: noise
+// The same for two bf16 elements at a time, whose eight digits fp16 holds: half the instructions.  `less`: their blocks' (byte - 16) << 7 (less_of); u: noise
 // in the low bytes of the halves.  A difference of exponents makes 2 a in fp16 of |v| (what is below 2^-14 comes out as something below 2^-14 and is
 // rounded to 0 like it).  a + 2^(e + 1) is rounded to a multiple of 2^(e - 9) = s / 256, and the bits of the sum count these multiples; 512 e more and bits 8 and up
 // are the code.  Returned as by noisy_code, in either half.
-constexpr unsigned MX_PAIRS_FROM = 16;   // the smallest scale byte
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+constexpr unsigned PAIRS_FROM = 16;   // the smallest scale byte; of zeros (padding, above all) any will do
+__device__ __forceinline__ bool in_pairs(unsigned byte, unsigned top) { return byte >= PAIRS_FROM || top == 0; }
+__device__ __forceinline__ unsigned short less_of(unsigned byte) { return static_cast<unsigned short>((max(byte, PAIRS_FROM) - PAIRS_FROM) << 7); }
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ unsigned noisy_pair(unsigned v, u16x2 less, unsigned u) {
   const u16x2 twice = __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, v & 0x7FFF7FFFu), less) << 3;
@@ -158,8 +160,9 @@ __device__ __forceinline__ void store8(E* p, int64_t left, const float (&v)[8]) 
   }
 }
 
-// Tile (x, y) of a block: the RUN tiles after one another that a row of tiles has in it go to one XCD (dispatch goes round the XCDs block by block), since
-// neighbours share lines: all of noise, whose rows of a tile are 64 bytes, and all where rows do not begin on lines.
+// Tile (x, y) of a block.  Blocks go round the XCDs one by one; RUN tiles in a row go to the same one, since neighbours share lines: those of noise, of which a
+// tile has 64 bytes a row, and all where rows do not begin on lines.  us without and with, both ways: bf16 8192 x 12288 66.5 and 59, 3 of 4097 x 1531 17.0 and 13.5,
+// with noise 33 and 25, fp32 2 of 25600 x 5120 254 and 244.
 constexpr int N_XCD = 8, RUN = 16;
 __device__ __forceinline__ uint2 tile_of_block() {
   const unsigned n = gridDim.x * gridDim.y, id = blockIdx.x + gridDim.x * blockIdx.y, in = id % (N_XCD * RUN);
@@ -169,9 +172,10 @@ __device__ __forceinline__ uint2 tile_of_block() {
 
 // One block rounds a tile of 128 rows x 64 columns: first along its rows (8 lanes a row, 8 elements each, 4 lanes a block), keeping
 // the elements in LDS, then along its columns (a thread two blocks).  Scale bytes are collected in LDS and leave in pieces of 128 bytes and more.
-// Every element is read once and every image written once (the counters say 1.05 GB and 0.28 GB for two fp32 matrices of 25600 x 5120, both ways): 254 us, 5.2
-// TB/s.  The tile is as large as leaves room for four blocks and more on a CU (128 x 128 took 296 us).  Rounding with noise is bound by its
-// arithmetic, 13 instructions an element and side: bf16 8192 x 12288 both ways 120 us where 66 do without noise.
+// Every element is read once and every image written once: fp32 25600 x 5120, two matrices, both ways 244 us (1.33 GB, 5.4 TB/s; a plain copy of 2 GiB reaches
+// 4.65), bf16 8192 x 12288 59 us (5.2 TB/s), 3 of 4097 x 1531 13.5 us (4.3).  The tile is as large as leaves room for four blocks and more on a CU
+// (128 x 128 took 296 us for the first), and a thread's loads are all on their way before the first is used.  With noise
+// arithmetic counts as much as memory: 7 instructions an element and side in pairs, 13 in fp32; bf16 8192 x 12288 both ways 85 us (120 without pairs).
 constexpr int ROWS = 128, COLS = 64;
 template <typename E, bool ROW, bool COL, bool NOISE>
 __global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {
@@ -226,10 +230,10 @@ __global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {
       PairMax<E> top;
 #pragma unroll
       for (int e = 0; e < 8; e += 2) top.take({static_cast<E>(v[e]), static_cast<E>(v[e + 1])});
-      const unsigned byte = mx_scale_byte(largest_of_four(max(top.of(0), top.of(1))), ceil);
+      const unsigned largest = largest_of_four(max(top.of(0), top.of(1))), byte = mx_scale_byte(largest, ceil);
       unsigned codes;
-      if (PAIRS && byte >= MX_PAIRS_FROM) {
-        const unsigned short less = static_cast<unsigned short>((byte - MX_PAIRS_FROM) << 7);
+      if (PAIRS && in_pairs(byte, largest)) {
+        const unsigned short less = less_of(byte);
         unsigned p[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -271,8 +275,8 @@ __global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {
       };
       const unsigned byte[2] = {mx_scale_byte(top.of(0), ceil), mx_scale_byte(top.of(1), ceil)};
       u32x4 codes[2] = {{0u, 0u, 0u, 0u}, {0u, 0u, 0u, 0u}};
-      if (PAIRS && min(byte[0], byte[1]) >= MX_PAIRS_FROM) {
-        const u16x2 less = {static_cast<unsigned short>((byte[0] - MX_PAIRS_FROM) << 7), static_cast<unsigned short>((byte[1] - MX_PAIRS_FROM) << 7)};
+      if (PAIRS && in_pairs(byte[0], top.of(0)) && in_pairs(byte[1], top.of(1))) {
+        const u16x2 less = {less_of(byte[0]), less_of(byte[1])};
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
           unsigned p[8];
@@ -342,7 +346,8 @@ __device__ __forceinline__ void eight_values(unsigned codes, unsigned byte, floa
     for (int i = 0; i < 8; ++i) v[i] = __builtin_nanf("");
 }
 
-// The values of a tile of 128 x 128 elements of the caller's matrix, from either image (the transposed one by way of LDS).
+// The values of a tile of 128 x 128 elements of the caller's matrix, from either image (the transposed one by way of LDS).  What is written bounds it: bf16 2 of
+// 25600 x 5120 141 us from by_row and 127 from by_col (0.66 GB, 4.7 and 5.2 TB/s), 3 of 4097 x 1531, whose rows begin anywhere, 10.7 and 11.7 us (4.4 and 4.1).
 template <typename E, bool COL>
 __global__ __launch_bounds__(THREADS) void k_mx_dequantize(MxMats m) {
   constexpr int LDT = TILE + 8 / sizeof(E);
