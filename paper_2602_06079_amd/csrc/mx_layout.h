@@ -43,7 +43,7 @@ constexpr int64_t mx_image_bytes(int64_t rows, int64_t k) {
   return mx_code_bytes(rows, k) + mx_row_tiles(rows) / 4 * mx_k_units(k) * MX_SCALE_BYTES;
 }
 
-// Launches take a block per tile of 128 x 128 or 64 x 64 elements and at most 2^32 threads: refused are matrices of more than 2^37 padded elements
+// Launches take a block per tile of 128 x 64 elements or more and at most 2^32 threads: refused are matrices of more than 2^37 padded elements
 // (no card holds one).
 constexpr bool mx_fits_grid(int64_t rows, int64_t cols) { return ((rows + 127) / 128) * ((cols + 127) / 128) <= (int64_t(1) << 37) / (128 * 128); }
 

@@ -343,6 +343,47 @@ def test_step_images_are_the_step_and_its_images(canz, out_dtype):
                     assert clean and np.array_equal(codes, want[0]) and np.array_equal(scales, want[1])
 
 
+def test_step_images_from_fragments_in_a_graph(canz):
+    """Gradients in two column fragments; the step with images recorded and replayed: after every replay the images are those of the parameters, which have
+    the bits of as many eager steps."""
+    import torch
+    hp = canz.Hparams()
+    rows, cols = 256, 512
+
+    def make():
+        grads = [torch.from_numpy(W.gen_grad(3, i, rows, cols)[0]).cuda() for i in range(2)]
+        frags = [f.contiguous() for g in grads for f in g.chunk(2, dim=1)]
+        out = [torch.from_numpy(W.gen_param(3, i, rows, cols)).to(torch.bfloat16).cuda() for i in range(2)]
+        return canz.Group(rows=rows, cols=cols, tp=2, grad=frags, mom=[torch.zeros(rows, cols, device="cuda") for _ in out], out=out, grad_dtype=W.DT_F32,
+                          out_dtype=W.DT_BF16)
+    a, b = make(), make()
+    ws = torch.empty(canz.canz_muon_workspace_bytes([a], hp), dtype=torch.uint8, device="cuda")
+    ws_b = torch.empty_like(ws)
+    img = lambda r, c: [torch.empty(canz.canz_mx_image_bytes(r, c), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    images = canz.MxImages(by_row=img(rows, cols), by_col=img(cols, rows))
+    call = lambda: canz.canz_muon_step_images([b], hp, [images], MX.FLOOR, ws_b, ws_b.numel(), stream())
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    canz.canz_muon_step([a], hp, ws, ws.numel(), stream())
+    for _ in range(3):
+        canz.canz_muon_step([a], hp, ws, ws.numel(), stream())
+        for t in images.by_row + images.by_col:
+            t.fill_(0x55)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for i in range(2):
+            assert torch.equal(a.out[i], b.out[i]) and torch.equal(a.mom[i], b.mom[i])
+            v = b.out[i].double().cpu().numpy()
+            for t, val in ((images.by_row[i], v), (images.by_col[i], v.T)):
+                codes, scales, clean = MX.unpack(t.cpu().numpy(), *val.shape)
+                want = MX.quantize(val, MX.FLOOR)
+                assert clean and np.array_equal(codes, want[0]) and np.array_equal(scales, want[1])
+
+
 def test_graph_replays_and_other_streams(canz):
     """Rounding and products of one and of many rows recorded into two graphs with workspaces of their own, replayed with eager work between,
     on inputs that change; and the same on a side stream."""
