@@ -6,6 +6,7 @@
 
 #include "canz.h"
 #include "mx_layout.h"
+#include "mx_rules.h"
 
 namespace canz {
 
@@ -47,9 +48,7 @@ hipError_t launch_mx_quantize(const MxMats& m, hipStream_t st);
 hipError_t launch_mx_dequantize(const MxMats& m, hipStream_t st);
 
 // C = alpha A B^T + beta C of images A (m x k) and B (n x k), several products in one launch.  A may also be a matrix, which the kernel rounds on
-// its way: with up to 16 rows, as long as every block rounding it again costs less than a launch that makes its image (4 us): 8 x 25600 x
-// 5120 18.4 us and 16.9 + 4, 16 x 25600 x 5120 22.7 and 15.2 + 4.5, 8 x 5120 x 25600 24.8 and 20.8 + 4.5, 8 x 4096 x 4096 5.9 and 4.5 + 4.
-constexpr bool mx_rounds_on_the_way(int64_t m, int64_t n, int64_t k) { return m <= 16 && m * n <= (int64_t(1) << 30) / (k > 0 ? k : 1); }
+// its way (mx_rounds_on_the_way).
 struct MxProblem {
   const uint8_t* a;   // image, or the matrix's first element
   const uint8_t* b;
@@ -61,20 +60,6 @@ struct MxProblem {
 };
 constexpr int MX_MAX_PROBLEMS = 32;
 
-// How many parts k is cut into, each a problem of its own with fp32 sums in the workspace, which launch_mx_join adds up: products of more than 64 rows whose
-// tiles leave most of the chip idle for long.  A unit of k takes a tile 210 ns, a second launch and the sums through memory up to 8 us.  us, whole and in
-// parts: 128 x 1024 x 65536 102 and 22.4, 100 x 1000 x 20000 35.5 and 14.4, 1024 x 1024 x 16384 29.5 and 24.2, 300 x 500 x 8000 17.9 and 13.2, 256 x 2048 x
-// 8192 17.1 and 14.4, 1024 x 1024 x 8192 17.5 and 17.2; not cut: 2048 x 1024 x 4096 11.6, 128 x 128 x 4096 10.2.  A product alone decides, so that its
-// sums do not depend on what shares the call.
-constexpr int MX_MAX_PARTS = 8;
-constexpr int mx_parts(int64_t m, int64_t n, int64_t k) {
-  if (m <= 64 || n == 0 || k == 0) return 1;
-  const int64_t tiles = ((m + 127) / 128) * ((n + 127) / 128), units = mx_k_units(k);
-  int64_t parts = 128 / tiles;
-  if (parts > MX_MAX_PARTS) parts = MX_MAX_PARTS;
-  if (parts > units / 8) parts = units / 8;
-  return parts >= 2 && (units - units / parts) * 210 >= 8000 ? static_cast<int>(parts) : 1;
-}
 struct MxProblems {
   int n;
   int first_tile[MX_MAX_PROBLEMS + 1];   // of every problem, then their number: set by the launcher, side by side, since every block goes through them

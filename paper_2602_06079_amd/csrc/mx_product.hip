@@ -112,7 +112,6 @@ __device__ __forceinline__ void store_piece(E* c, int64_t left, i32x4 v) {
 //
 // The operand layout gives a lane 32 consecutive elements of one row, a block: a matrix A is rounded by the lane that needs it, without
 // a word to another one, so that a call of few rows is one launch.
-constexpr int FEW_ROWS = 64;
 
 // the operand of one lane: 32 elements and their scale byte
 struct Block {
@@ -658,19 +657,6 @@ int64_t count_tiles(MxProblems& ps, int rows, int cols) {
   return tiles;
 }
 
-constexpr int N_CU = 256;
-
-// ns that a launch takes by the tiles it has: 256 x 256 in rounds of one to a CU, 128 x 128 in rounds of two, or less than one at the end.  A k unit
-// takes 780 ns of a round of large tiles and 460 of one of small ones (a quarter of the work, twice as often), 210 with one small tile to a CU; beginning
-// and end of a tile 6000 and 2600.  us for bf16 results, 256 x 256 and 128 x 128: 8192^3 223, 252; 4096^3 35, 36; 8192 x 12288 x 4096 189, 213; 4096 x
-// 25600 x 5120 246, 256; 6000 x 6000 x 2000 52, 42; 5000 x 4000 x 1000 28, 19; 4096 x 4096 x 1024 18.1, 16.8; 3000^3 25, 21; 2048 x 4096 x 8192 49, 35;
-// 4096 x 2048 x 1024 15.7, 10.8; 1024^3 13.6, 6.3.
-int64_t large_tiles_ns(int64_t tiles, int64_t ks) { return (tiles + N_CU - 1) / N_CU * (780 * ks + 6000); }
-int64_t small_tiles_ns(int64_t tiles, int64_t ks) {
-  const int64_t rest = tiles % (2 * N_CU);
-  return tiles / (2 * N_CU) * (460 * ks + 2600) + (rest > N_CU ? 460 * ks + 2600 : rest > 0 ? 210 * ks + 2600 : 0);
-}
-
 // blocks for these tiles, `most` (a multiple of 8) at a time: as many on each XCD as the one with most tiles has
 dim3 tile_grid(const MxProblems& ps, int most) {
   int64_t longest = 0;   // an XCD has at most an eighth of each product, rounded up
@@ -697,7 +683,7 @@ hipError_t launch_tiles(MxProblems& ps, hipStream_t st) {
   int64_t units = 0;   // of all small tiles along k
   for (int i = 0; i < ps.n; ++i) units += static_cast<int64_t>(ps.first_tile[i + 1] - ps.first_tile[i]) * ps.pr[i].units;
   const int64_t ks = (units + small - 1) / small;
-  if (large_tiles_ns(large, ks) < small_tiles_ns(small, ks)) {
+  if (mx_large_tiles(large, small, ks)) {
     launch_large_tiles<float, false>(ps, st);
     launch_large_tiles<__bf16, false>(ps, st);
     launch_large_tiles<float, true>(ps, st);
@@ -714,13 +700,6 @@ hipError_t launch_few_as(MxProblems& ps, hipStream_t st) {
   k_mx_product_few<A, UM, UN, WAVES, AHEAD><<<dim3(static_cast<unsigned>(blocks)), 64 * WAVES, 0, st>>>(ps);
   return hipGetLastError();
 }
-
-// How the kernel for few rows goes over B, by its rows (a product alone decides, so that its sums do not depend on what shares the launch):
-// many of them are taken 64 to a block of four wavefronts, which halves what is read and rounded of A; with fewer the blocks are made smaller to fill the chip, and
-// with very few a block takes more wavefronts, so that k is gone through faster.  us for one row of bf16, 64 rows / 32 rows / 32 rows with 16 wavefronts:
-// 25600 x 5120 16.4 / 18.5 / 21.4, 12288 x 4096 6.9 / 7.5 / 8.2, 8192 x 5120 6.8 / 6.4 / 6.5, 5120 x 25600 24.1 / 19.2 / 20.1, 333 x 9000 9.2 / 8.0 / 6.8.
-enum Width { NARROW, MIDDLE, WIDE, WIDTHS };
-Width width_of(int64_t n) { return n >= 12288 ? WIDE : n >= 4096 ? MIDDLE : NARROW; }
 
 template <typename A, int UM, int AHEAD>
 hipError_t launch_few(MxProblems& ps, Width width, hipStream_t st) {
