@@ -478,7 +478,7 @@ int canz_muon_step_static(const canz_group* g, int32_t n_groups, const canz_muon
  * 4194240 each and padded matrices at most 2^37 elements; an extent may be 0, and then nothing is read or written (k = 0 in a product:
  * C <- beta C) and the pointers of that matrix may be NULL.  Tables are host arrays of device pointers, read during the call.
  * The calls issue kernel launches only (no allocation, copy, memset or synchronisation), on the device hip_stream
- * belongs to (NULL: the current one), and may be recorded into a HIP graph.  What a call writes must not overlap any other buffer of the call; what
+ * belongs to (NULL, hipStreamLegacy and hipStreamPerThread: the current one), and may be recorded into a HIP graph.  What a call writes must not overlap any other buffer of the call; what
  * it only reads may be given any number of times.  Results do not depend on what else is in the call.
  */
 enum { CANZ_MX_SCALE_FLOOR = 0, CANZ_MX_SCALE_CEIL = 1 };

@@ -10,12 +10,16 @@
 
 namespace canz {
 
+// The stream that a caller named.  The legacy default stream is the null stream by another name, and the runtime is only given that one: a call with the
+// handle of the former ended the process inside it.
+inline hipStream_t stream_of(void* named) { return named == hipStreamLegacy ? nullptr : static_cast<hipStream_t>(named); }
+
 // Kernels are launched on the device the caller's stream belongs to, whatever the thread's current device is.
 class StreamDevice {
  public:
   explicit StreamDevice(hipStream_t st) {
     hipDevice_t dev = 0;
-    if (st == nullptr) return;   // the null stream belongs to the current device
+    if (st == nullptr || st == hipStreamPerThread) return;   // these are the current device's
     if ((err_ = hipStreamGetDevice(st, &dev)) != hipSuccess || (err_ = hipGetDevice(&before_)) != hipSuccess) return;
     if (dev != before_) restore_ = (err_ = hipSetDevice(dev)) == hipSuccess;
   }

@@ -135,7 +135,7 @@ extern "C" int canz_mx_quantize(const canz_mx_group* g, int32_t n_groups, int32_
   if (int rc = check_scale_mode(scale_mode)) return rc;
   for (int i = 0; i < n_groups; ++i)
     if (int rc = check_mx_group(g[i], i, false)) return rc;
-  const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  const hipStream_t st = stream_of(hip_stream);
   const StreamDevice on(st);
   if (on.error() != hipSuccess) return fail(CANZ_EHIP, "stream: %s", hipGetErrorString(on.error()));
   for (int i = 0; i < n_groups; ++i)
@@ -148,7 +148,7 @@ extern "C" int canz_mx_dequantize(const canz_mx_group* g, int32_t n_groups, void
   if (n_groups < 0 || (n_groups > 0 && !g)) return fail(CANZ_EINVAL, "bad group array");
   for (int i = 0; i < n_groups; ++i)
     if (int rc = check_mx_group(g[i], i, true)) return rc;
-  const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  const hipStream_t st = stream_of(hip_stream);
   const StreamDevice on(st);
   if (on.error() != hipSuccess) return fail(CANZ_EHIP, "stream: %s", hipGetErrorString(on.error()));
   for (int i = 0; i < n_groups; ++i) {
@@ -182,7 +182,7 @@ extern "C" int canz_mx_product(const canz_mx_product_group* g, int32_t n_groups,
   size_t need = 0;
   if (int rc = product_workspace(g, n_groups, &need)) return rc;
   if (workspace_bytes < need) return fail(CANZ_EWORKSPACE, "workspace too small: %zu bytes given, %zu needed", workspace_bytes, need);
-  const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  const hipStream_t st = stream_of(hip_stream);
   const StreamDevice on(st);
   if (on.error() != hipSuccess) return fail(CANZ_EHIP, "stream: %s", hipGetErrorString(on.error()));
 
@@ -271,7 +271,7 @@ extern "C" int canz_muon_step_images(const canz_group* g, int32_t n_groups, cons
   if (!hp) return fail(CANZ_EINVAL, "null hparams");
   if (hp->out_mode != CANZ_OUT_PARAM) return fail(CANZ_EUNSUPPORTED, "images are taken of updated parameters: out_mode must be CANZ_OUT_PARAM");
   if (int rc = check_scale_mode(scale_mode)) return rc;
-  const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  const hipStream_t st = stream_of(hip_stream);
   const StreamDevice on(st);
   if (on.error() != hipSuccess) return fail(CANZ_EHIP, "stream: %s", hipGetErrorString(on.error()));
   // everything is checked before the step is enqueued; the second time round the images are
@@ -286,7 +286,7 @@ extern "C" int canz_muon_step_images(const canz_group* g, int32_t n_groups, cons
       if (rc) return rc;
     }
     if (pass == 1) return CANZ_OK;
-    if (int rc = canz_muon_step(g, n_groups, hp, workspace, workspace_bytes, hip_stream)) return rc;
+    if (int rc = canz_muon_step(g, n_groups, hp, workspace, workspace_bytes, st)) return rc;
   }
   return CANZ_OK;
 }
