@@ -161,8 +161,9 @@ __device__ __forceinline__ void store8(E* p, int64_t left, const float (&v)[8]) 
 }
 
 // Tile (x, y) of a block.  Blocks go round the XCDs one by one; RUN tiles in a row go to the same one, since neighbours share lines: those of noise, of which a
-// tile has 64 bytes a row, and all where rows do not begin on lines.  us without and with, both ways: bf16 8192 x 12288 66.5 and 59, 3 of 4097 x 1531 17.0 and 13.5,
-// with noise 33 and 25, fp32 2 of 25600 x 5120 254 and 244.
+// tile has 64 bytes a row, and all where rows do not begin on lines.  us without and with, both ways: bf16 8192 x 12288 66.6 and 59.0, 3 of 4097 x 1531 17.2 and 13.6,
+// with noise 29.6 and 23.2, fp32 2 of 25600 x 5120 255 and 243.  (Here and below launches follow each other on three sets of buffers in turn; alone under a profiler a
+// launch takes up to a quarter longer.)
 constexpr int N_XCD = 8, RUN = 16;
 __device__ __forceinline__ uint2 tile_of_block() {
   const unsigned n = gridDim.x * gridDim.y, id = blockIdx.x + gridDim.x * blockIdx.y, in = id % (N_XCD * RUN);
@@ -172,10 +173,11 @@ __device__ __forceinline__ uint2 tile_of_block() {
 
 // One block rounds a tile of 128 rows x 64 columns: first along its rows (8 lanes a row, 8 elements each, 4 lanes a block), keeping
 // the elements in LDS, then along its columns (a thread two blocks).  Scale bytes are collected in LDS and leave in pieces of 128 bytes and more.
-// Every element is read once and every image written once: fp32 25600 x 5120, two matrices, both ways 244 us (1.33 GB, 5.4 TB/s; a plain copy of 2 GiB reaches
-// 4.65), bf16 8192 x 12288 59 us (5.2 TB/s), 3 of 4097 x 1531 13.5 us (4.3).  The tile is as large as leaves room for four blocks and more on a CU
+// Every element is read once and every image written once: fp32 25600 x 5120, two matrices, both ways 243 us (1.33 GB, 5.4 TB/s; a plain copy of 2 GiB, half of it
+// writes, reaches 4.65 to 4.95), bf16 8192 x 12288 59 us (5.2 TB/s), 3 of 4097 x 1531 13.6 us (4.2).  The tile is as large as leaves room for four blocks and more on a CU
 // (128 x 128 took 296 us for the first), and a thread's loads are all on their way before the first is used.  With noise
-// arithmetic counts as much as memory: 7 instructions an element and side in pairs, 13 in fp32; bf16 8192 x 12288 both ways 85 us (120 without pairs).
+// arithmetic counts as much as memory: 7 instructions an element and side in pairs, 13 in fp32; both ways bf16 8192 x 12288 88 us (120 without pairs; 4.6 TB/s),
+// fp32 123 us (5.0), two of fp32 25600 x 5120 321 us (5.0).
 constexpr int ROWS = 128, COLS = 64;
 template <typename E, bool ROW, bool COL, bool NOISE>
 __global__ __launch_bounds__(THREADS) void k_mx_quantize(MxMats m) {
@@ -348,6 +350,7 @@ __device__ __forceinline__ void eight_values(unsigned codes, unsigned byte, floa
 
 // The values of a tile of 128 x 128 elements of the caller's matrix, from either image (the transposed one by way of LDS).  What is written bounds it: bf16 2 of
 // 25600 x 5120 141 us from by_row and 127 from by_col (0.66 GB, 4.7 and 5.2 TB/s), 3 of 4097 x 1531, whose rows begin anywhere, 10.7 and 11.7 us (4.4 and 4.1).
+// fp32: 337 and 255 us (3.5 and 4.65 TB/s), 17.7 and 21.6 us (4.8 and 4.0).
 template <typename E, bool COL>
 __global__ __launch_bounds__(THREADS) void k_mx_dequantize(MxMats m) {
   constexpr int LDT = TILE + 8 / sizeof(E);

@@ -43,8 +43,8 @@ constexpr int64_t mx_image_bytes(int64_t rows, int64_t k) {
   return mx_code_bytes(rows, k) + mx_row_tiles(rows) / 4 * mx_k_units(k) * MX_SCALE_BYTES;
 }
 
-// Launches take a block per tile of 128 x 64 elements or more and at most 2^32 threads: refused are matrices of more than 2^37 padded elements
-// (no card holds one).
+// Launches take a block of 256 threads per tile of 128 x 64 elements or more and stay below 2^32 threads for one matrix: refused are matrices of more than
+// 2^37 padded elements (73 GB as an image, 275 GB in bf16).
 constexpr bool mx_fits_grid(int64_t rows, int64_t cols) { return ((rows + 127) / 128) * ((cols + 127) / 128) <= (int64_t(1) << 37) / (128 * 128); }
 
 }  // namespace canz

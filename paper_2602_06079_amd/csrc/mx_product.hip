@@ -388,6 +388,7 @@ __global__ __launch_bounds__(THREADS) void k_mx_scale(MxProblem p) {
 // take 157 us (7.0 PFLOP/s, 1.83 GHz).  Left out one by one, requests from L2 into LDS make 48 us of it, reads from LDS 18, stores 15.  (32 x 32 x 64
 // instructions reach 6.2 PFLOP/s from registers, 16 x 16 x 128 ones 7.0: that is why images are laid out for the latter.)
 // So W instructions after one another keep their second operand and change the first: with the first one kept 8192 x 12288 x 4096 takes 215 us instead of 198.
+// Old results cost their bytes and the waiting for them behind a tile: 8192 x 4096 x 12288 bf16 180 us without and 206 with, fp32 188 and 210.
 constexpr int BAND = 4;   // tile rows that are walked column by column: 8192^3 233 us, with 2 or 16 of them 238; 4096 x 25600 x 5120 266, 267 and 261
 
 template <int W>

@@ -39,7 +39,8 @@ constexpr Width width_of(int64_t n) { return n >= 12288 ? WIDE : n >= 4096 ? MID
 // tiles leave most of the chip idle for long.  A unit of k takes a tile 210 ns, a second launch and the sums through memory up to 8 us.  us, whole and in
 // parts: 128 x 1024 x 65536 102 and 22.4, 100 x 1000 x 20000 35.5 and 14.4, 1024 x 1024 x 16384 29.5 and 24.2, 300 x 500 x 8000 17.9 and 13.2, 256 x 2048 x
 // 8192 17.1 and 14.4, 1024 x 1024 x 8192 17.5 and 17.2; not cut: 2048 x 1024 x 4096 11.6, 128 x 128 x 4096 10.2.  A product alone decides, so that its
-// sums do not depend on what shares the call.
+// sums do not depend on what shares the call.  Not cut either, whatever k: products of 65 and more tiles, which run on up to half of the chip (1024 x 2048 x
+// 65536 138 us), and those of up to 64 rows, whose blocks have 32 or 64 columns each (64 x 1024 x 65536 35.7, 64 x 1000 x 20000 13.3).
 constexpr int MX_MAX_PARTS = 8;
 constexpr int mx_parts(int64_t m, int64_t n, int64_t k) {
   if (m <= 64 || n == 0 || k == 0) return 1;
