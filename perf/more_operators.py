@@ -1,0 +1,440 @@
+"""Performance cases: what lies between an updated weight matrix and its next gradient: the norm in front of a linear layer, activations kept in
+8 bits for the backward pass, and the layer's products in bf16.
+
+An 8-bit image holds a matrix as MXFP8: blocks of 32 consecutive elements of a row share a power of two X, the smallest one of 2^-124 and above
+with amax <= 448 X for the largest magnitude amax of the block, and an element is the nearest value of E4M3 (4 significant bits down to 2^-6, the
+spacing 2^-9 below, at most 448) times X, ties to the even code.
+
+  op "norm"     y = w h / sqrt(mean(h^2) + eps) over the rows of h = x + residual (rounded to the type of the residual); y as bf16 and as an 8-bit image
+                ("serve"), or with the gradients for x and w ("train"), the backward pass from h ("sum") or from an 8-bit image of h ("8bit")
+                rows, cols; sum "bf16" | "f32": type of the residual stream; mode "serve" | "train"; kept "sum" | "8bit"
+  op "gate"     out = act(gate) up (or act(gate) alone), gate and up kept in 8 bits; the gradients for both and out once more from these images
+                rows, cols; act "silu" | "gelu" | "relu"; up 0 | 1; dtype "bf16" | "f32"
+  op "keep"     matrices -> 8-bit images -> their values
+                rows, cols, count; dtype "bf16" | "f32"
+  op "linear"   act(x W^T + bias) + residual; x in bf16 or as an 8-bit image
+                m "1" or "<rows>+<rows>+...": one product for each part of x, with a W of its own (experts; a part may be empty)
+                n, k; x "bf16" | "8bit"; out "bf16" | "f32"; bias, residual, pre (the value in front of act kept in 8 bits, too) 0 | 1; act
+                "none" | "silu" | "gelu" | "relu"
+  op "layer"    training pass of a linear layer: y = x W^T + bias and dx = dy W in bf16, dW = dy^T x and the bias' gradient in fp32, x from its 8-bit image
+                tokens, n, k
+
+Shapes are those of this repository's workloads (paper_2602_06079_amd/workloads.py) and generic odd ones.
+"""
+import math
+
+import torch
+
+own = False
+
+DEV = "cuda"
+BLOCK = 32
+EPS = 1e-6
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def listed():
+    return [
+        # one token between two blocks of a 0.6B-shaped model: latency
+        dict(name="norm_token", op="norm", rows=1, cols=1024, sum="bf16", mode="serve", kept="sum"),
+        # training tokens of an 8B-shaped model, forward and backward
+        dict(name="norm_8b", op="norm", rows=8192, cols=4096, sum="bf16", mode="train", kept="sum"),
+        # odd extents, fp32 residual stream, its 8-bit image kept
+        dict(name="norm_ragged", op="norm", rows=4097, cols=1531, sum="f32", mode="train", kept="8bit"),
+        # a few tokens through an activation without a gate
+        dict(name="gate_few", op="gate", rows=37, cols=1000, act="gelu", up=0, dtype="bf16"),
+        # training tokens between gate / up and down of an 8B-shaped model, forward and backward
+        dict(name="gate_8b", op="gate", rows=8192, cols=12288, act="silu", up=1, dtype="bf16"),
+        # activations of two layers put away in fp32 and fetched again
+        dict(name="keep_32b", op="keep", rows=8192, cols=5120, count=2, dtype="f32"),
+        # one token through the 32B-shaped down projection, onto the residual stream: the weights are read once
+        dict(name="linear_token", op="linear", m="1", n=5120, k=25600, x="bf16", out="bf16", bias=0, residual=1, pre=0, act="none"),
+        # a small batch of sequences, one token each, from the norm's 8-bit output
+        dict(name="linear_few", op="linear", m="17", n=25600, k=5120, x="8bit", out="bf16", bias=0, residual=0, pre=0, act="silu"),
+        # a prompt through the 32B-shaped gate, with a bias and an activation whose argument is kept
+        dict(name="linear_prompt", op="linear", m="4096", n=25600, k=5120, x="bf16", out="bf16", bias=1, residual=0, pre=1, act="gelu"),
+        # odd extents, everything in the epilogue
+        dict(name="linear_odd", op="linear", m="777", n=1531, k=1000, x="bf16", out="f32", bias=1, residual=1, pre=1, act="gelu"),
+        # experts with the tokens a router gave them, two of them none
+        dict(name="linear_experts", op="linear", m="0+1+37+400+5+128+0+1000", n=1536, k=4096, x="bf16", out="bf16", bias=0, residual=0, pre=0, act="silu"),
+        # training pass of an 8B-shaped gate
+        dict(name="layer_8b", op="layer", tokens=8192, n=12288, k=4096),
+    ]
+
+
+def draw(rng):
+    """One more case of the same ranges: sizes spread over their logarithm, odd ones among them."""
+    def extent(lo, hi):
+        x = int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+        kind = rng.random()
+        if kind < 0.3:
+            x = max(1, round(x / 256)) * 256
+        elif kind < 0.6:
+            x = max(1, round(x / 32)) * 32
+        return max(lo, min(hi, x))
+
+    op = rng.choice(["norm", "gate", "keep", "linear", "linear", "linear", "layer"])
+    if op == "norm":
+        rows, cols = extent(1, 8192), extent(64, 25600)
+        rows = min(rows, (1 << 25) // cols)
+        return dict(op=op, rows=rows, cols=cols, sum=rng.choice(["bf16", "f32"]), mode=rng.choice(["serve", "train", "train"]),
+                    kept=rng.choice(["sum", "8bit"]))
+    if op == "gate":
+        rows, cols = extent(1, 8192), extent(64, 25600)
+        rows = min(rows, (1 << 26) // cols)
+        return dict(op=op, rows=rows, cols=cols, act=rng.choice(["silu", "silu", "gelu", "relu"]), up=rng.choice([0, 1, 1]),
+                    dtype=rng.choice(["bf16", "bf16", "f32"]))
+    if op == "keep":
+        rows, cols = extent(1, 8192), extent(33, 25600)
+        return dict(op=op, rows=rows, cols=cols, count=rng.randint(1, max(1, min(16, (1 << 26) // (rows * cols)))), dtype=rng.choice(["bf16", "f32"]))
+    if op == "layer":
+        tokens, n, k = extent(33, 8192), extent(64, 12288), extent(64, 12288)
+        while tokens * n * k > 8192 * 12288 * 4096:
+            tokens, n, k = (max(33, e // 2) for e in (tokens, n, k))
+        return dict(op=op, tokens=tokens, n=n, k=k)
+    n, k = extent(33, 25600), extent(33, 25600)
+    kind = rng.choice(["one", "few", "many", "experts"])
+    if kind == "experts":
+        n, k = min(n, 4096), min(k, 4096)
+        m = "+".join(str(rng.choice([0, 1, rng.randint(2, 64), extent(33, 1000)])) for _ in range(rng.randint(2, 12)))
+        m += "+%d" % rng.randint(1, 64)
+    else:
+        m = 1 if kind == "one" else rng.randint(2, 64) if kind == "few" else extent(65, 4096)
+        m = str(max(1, min(m, 4096 * 25600 * 5120 // (n * k))))
+    return dict(op=op, m=m, n=n, k=k, x=rng.choice(["bf16", "bf16", "8bit"]), out=rng.choice(["bf16", "bf16", "f32"]), bias=rng.randint(0, 1),
+                residual=rng.randint(0, 1), pre=rng.randint(0, 1), act=rng.choice(["none", "silu", "gelu", "relu"]))
+
+
+def _gen(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(int(seed))
+    return g
+
+
+def _normal(g, rows, cols, dtype, scale=1.0):
+    return (torch.randn(rows, cols, device=DEV, generator=g) * scale).to(dtype)
+
+
+def _hidden(g, rows, cols):
+    """Rows as they come out of a block: Gaussian with a few strong channels (fp32)."""
+    x = torch.randn(rows, cols, device=DEV, generator=g)
+    x *= torch.where(torch.rand(cols, device=DEV, generator=g) < 0.01, 20.0, 1.0)
+    return x
+
+
+def _parts(case):
+    return [int(m) for m in case["m"].split("+")]
+
+
+def prepare(case, seed):
+    g = _gen(seed)
+    s = dict(case=case)
+    bf16 = torch.bfloat16
+    if case["op"] == "norm":
+        r, c, st = case["rows"], case["cols"], DTYPES[case["sum"]]
+        s["x"], s["residual"] = _normal(g, r, c, bf16), _hidden(g, r, c).to(st)
+        s["w"] = 1 + 0.1 * torch.randn(c, device=DEV, generator=g)
+        if case["mode"] == "train":
+            s["dy"], s["dsum"] = _normal(g, r, c, bf16, 1e-3), _normal(g, r, c, st, 1e-3)
+    elif case["op"] == "gate":
+        r, c, dt = case["rows"], case["cols"], DTYPES[case["dtype"]]
+        s["gate"] = _normal(g, r, c, dt, 2.0)
+        s["up"] = _normal(g, r, c, dt) if case["up"] else None
+        s["dout"] = _normal(g, r, c, dt, 1e-3)
+    elif case["op"] == "keep":
+        s["x"] = [_hidden(g, case["rows"], case["cols"]).to(DTYPES[case["dtype"]]) for _ in range(case["count"])]
+    elif case["op"] == "linear":
+        ms, n, k, out = _parts(case), case["n"], case["k"], DTYPES[case["out"]]
+        s["x"] = [_held(_hidden(g, m, k)) if case["x"] == "8bit" else _hidden(g, m, k).to(bf16) for m in ms]
+        s["w"] = [_normal(g, n, k, bf16, k ** -0.5) for _ in ms]
+        s["bias"] = [0.5 * torch.randn(n, device=DEV, generator=g) for _ in ms] if case["bias"] else []
+        s["residual"] = [_normal(g, m, n, out) for m in ms] if case["residual"] else []
+    else:
+        t, n, k = case["tokens"], case["n"], case["k"]
+        s["x"], s["dy"] = _held(_hidden(g, t, k)), _normal(g, t, n, bf16, 1e-3)
+        s["w"], s["bias"] = _normal(g, n, k, bf16, k ** -0.5), 0.5 * torch.randn(n, device=DEV, generator=g)
+    if own:
+        _keep(s)
+    return s
+
+
+def run(s):
+    return _run_own(s) if own else _run_plain(s)
+
+
+# ---------------------------------------------------------------- plain form
+
+def _eight(x):
+    """The values that the 8-bit image of a matrix stands for (fp32)."""
+    rows, k = x.shape
+    blocks = -(-k // BLOCK)
+    v = torch.nn.functional.pad(x.float(), (0, -k % BLOCK)).view(rows, blocks, BLOCK)
+    mant, exp = torch.frexp(v.abs().amax(-1, keepdim=True))      # amax = mant 2^exp, mant in [0.5, 1); 448 = 0.875 2^9
+    e = (exp - 9 + (mant > 0.875).int()).clamp(min=-124)
+    a = torch.ldexp(v, -e)
+    _, ea = torch.frexp(a)
+    step = (ea - 1).clamp(min=-6) - 3
+    q = torch.ldexp(torch.round(torch.ldexp(a, -step)), step + e)
+    return q.view(rows, blocks * BLOCK)[:, :k]
+
+
+def _held(x):
+    """The same as a program keeps them: bf16 holds these values exactly."""
+    return _eight(x).to(torch.bfloat16).contiguous()
+
+
+def _act(name, z):
+    """act(z) and its derivative."""
+    if name == "none":
+        return z, torch.ones_like(z)
+    if name == "relu":
+        return z.clamp(min=0), (z > 0).to(z.dtype)
+    if name == "silu":
+        p = 1 / (1 + torch.exp(-z))
+        return z * p, p * (1 + z * (1 - p))
+    p = 0.5 * torch.erfc(z * -(0.5 ** 0.5))
+    return z * p, p + z * torch.exp(-0.5 * z * z) * (2 * math.pi) ** -0.5
+
+
+def _run_plain(s):
+    c = s["case"]
+    bf16 = torch.bfloat16
+    if c["op"] == "norm":
+        st, w = DTYPES[c["sum"]], s["w"]
+        total = (s["x"].float() + s["residual"].float()).to(st)
+        h = total.float()
+        rstd = torch.rsqrt(h.square().mean(1, keepdim=True) + EPS)
+        y = h * rstd * w
+        if c["mode"] == "serve":
+            return dict(sum=total, y=y.to(bf16), y8=_eight(y).to(bf16))
+        h = _eight(h) if c["kept"] == "8bit" else h
+        hn, dy = h * rstd, s["dy"].float()
+        u = w * dy
+        dx = s["dsum"].float() + rstd * (u - hn * (u * hn).mean(1, keepdim=True))
+        return dict(sum=total, y=y.to(bf16), rstd=rstd[:, 0], dx=dx.to(st), dw=(dy * hn).sum(0))
+    if c["op"] == "gate":
+        dt = DTYPES[c["dtype"]]
+        a, _ = _act(c["act"], s["gate"].float())
+        out = a * s["up"].float() if c["up"] else a
+        a, da = _act(c["act"], _eight(s["gate"]))
+        dout = s["dout"].float()
+        if not c["up"]:
+            return dict(out=out.to(dt), again=a.to(dt), dgate=(dout * da).to(dt))
+        up = _eight(s["up"])
+        return dict(out=out.to(dt), again=(a * up).to(dt), dgate=(dout * up * da).to(dt), dup=(dout * a).to(dt))
+    if c["op"] == "keep":
+        return [_eight(x).to(x.dtype) for x in s["x"]]
+    if c["op"] == "linear":
+        out = DTYPES[c["out"]]
+        z = [torch.matmul(x.float(), w.float().t()) for x, w in zip(s["x"], s["w"])]
+        z = [v + b for v, b in zip(z, s["bias"])] if c["bias"] else z
+        y = [_act(c["act"], v)[0] for v in z]
+        y = [v + r.float() for v, r in zip(y, s["residual"])] if c["residual"] else y
+        return dict(y=[v.to(out) for v in y], pre=[_eight(v).to(bf16) for v in z] if c["pre"] else [])
+    x, dy, w = s["x"].float(), s["dy"].float(), s["w"].float()
+    return dict(y=(torch.matmul(x, w.t()) + s["bias"]).to(bf16), dx=torch.matmul(dy, w).to(bf16), dw=torch.matmul(dy.t(), x), db=dy.sum(0))
+
+
+# ------------------------------------------------------- the framework's operators
+
+def _keep(s):
+    """What a program keeps from call to call: output buffers, images of what an earlier call left in 8 bits, groups, workspace."""
+    from paper_2602_06079_amd import binding as canz
+    c = s["case"]
+    dt = dict(f32=canz.DT_F32, bf16=canz.DT_BF16)
+    act = dict(none=canz.ACT_NONE, silu=canz.ACT_SILU, gelu=canz.ACT_GELU, relu=canz.ACT_RELU)
+    stream = torch.cuda.current_stream().cuda_stream
+    bf16 = torch.bfloat16
+
+    def image(rows, cols):
+        return torch.empty(max(256, canz.canz_mx8_bytes(rows, cols)), dtype=torch.uint8, device=DEV)
+
+    def stored(x):
+        im = image(*x.shape)
+        canz.canz_mx8_store([canz.Mx8Group(rows=x.shape[0], cols=x.shape[1], mat=[x], image=[im], dtype=canz.DT_BF16)], stream)
+        return im
+
+    def empty(rows, cols, dtype):
+        return torch.empty(rows, cols, dtype=dtype, device=DEV)
+
+    s["canz"], need = canz, 0
+    if c["op"] == "norm":
+        r, cc, st, sd = c["rows"], c["cols"], DTYPES[c["sum"]], dt[c["sum"]]
+        s["out"] = o = dict(sum=empty(r, cc, st), y=empty(r, cc, bf16))
+        common = dict(rows=r, cols=cc, dtype=canz.DT_BF16, sum_dtype=sd, weight_dtype=canz.DT_F32)
+        forward = dict(common, x=s["x"], residual=s["residual"], weight=s["w"], sum=o["sum"], y=o["y"], eps=EPS)
+        if c["mode"] == "serve":
+            im, o["y8"] = image(r, cc), empty(r, cc, bf16)
+            s["forward"] = [canz.Norm(y8=im, **forward)]
+            s["back"] = [canz.Mx8Group(rows=r, cols=cc, mat=[o["y8"]], image=[im], dtype=canz.DT_BF16)]
+        else:
+            o.update(rstd=torch.empty(r, device=DEV), dx=empty(r, cc, st), dw=torch.empty(cc, device=DEV))
+            s["forward"] = [canz.Norm(rstd=o["rstd"], **forward)]
+            eight = c["kept"] == "8bit"
+            im = image(r, cc) if eight else None
+            s["store"] = [canz.Mx8Group(rows=r, cols=cc, mat=[o["sum"]], image=[im], dtype=sd)] if eight else []
+            s["backward"] = [canz.NormGrad(dy=s["dy"], h=im if eight else o["sum"], h_dtype=canz.DT_MX8 if eight else sd, rstd=o["rstd"], weight=s["w"],
+                                           dsum=s["dsum"], dx=o["dx"], dweight=o["dw"], **common)]
+            need = canz.canz_norm_backward_workspace_bytes(s["backward"])
+    elif c["op"] == "gate":
+        r, cc, t, d = c["rows"], c["cols"], DTYPES[c["dtype"]], dt[c["dtype"]]
+        s["out"] = o = {name: empty(r, cc, t) for name in ("out", "again", "dgate") + (("dup",) if c["up"] else ())}
+        g8, u8 = image(r, cc), image(r, cc) if c["up"] else None
+        s["forward"] = [canz.Act(rows=r, cols=cc, gate=s["gate"], up=s["up"], out=o["out"], gate8=g8, up8=u8, act=act[c["act"]], dtype=d)]
+        s["backward"] = [canz.ActGrad(rows=r, cols=cc, dout=s["dout"], gate=g8, up=u8, out=o["again"], dgate=o["dgate"], dup=o.get("dup"),
+                                      act=act[c["act"]], dtype=d, in_dtype=canz.DT_MX8)]
+    elif c["op"] == "keep":
+        r, cc, count, d = c["rows"], c["cols"], c["count"], dt[c["dtype"]]
+        im = [image(r, cc) for _ in range(count)]
+        s["out"] = [torch.empty_like(x) for x in s["x"]]
+        s["store"] = [canz.Mx8Group(rows=r, cols=cc, mat=s["x"], image=im, dtype=d)]
+        s["back"] = [canz.Mx8Group(rows=r, cols=cc, mat=s["out"], image=im, dtype=d)]
+    elif c["op"] == "linear":
+        n, k, out = c["n"], c["k"], DTYPES[c["out"]]
+        eight = c["x"] == "8bit"
+        ms = [x.shape[0] for x in s["x"]]
+        x = [stored(v) if eight else v for v in s["x"]]
+        y = [empty(m, n, out) for m in ms]
+        pre = [image(m, n) for m in ms] if c["pre"] else []
+        s["out"] = dict(y=y, pre=[empty(m, n, bf16) for m in ms] if c["pre"] else [])
+        at = lambda v, i: v[i:i + 1]  # noqa: E731
+        s["groups"] = [canz.Linear(m=m, n=n, k=k, a=[x[i]], b=[s["w"][i]], c=[y[i]], bias=at(s["bias"], i), residual=at(s["residual"], i), pre8=at(pre, i),
+                                   a_dtype=canz.DT_MX8 if eight else canz.DT_BF16, out_dtype=dt[c["out"]], act=act[c["act"]],
+                                   beta=float(c["residual"])) for i, m in enumerate(ms)]
+        s["back"] = [canz.Mx8Group(rows=m, cols=n, mat=[v], image=[p], dtype=canz.DT_BF16) for m, v, p in zip(ms, s["out"]["pre"], pre)]
+        need = canz.canz_linear_workspace_bytes(s["groups"])
+    else:
+        t, n, k = c["tokens"], c["n"], c["k"]
+        x8 = stored(s["x"])
+        s["out"] = o = dict(y=empty(t, n, bf16), dx=empty(t, k, bf16), dw=empty(n, k, torch.float32), db=torch.empty(n, device=DEV))
+        s["groups"] = [canz.Linear(m=t, n=n, k=k, a=[x8], b=[s["w"]], c=[o["y"]], bias=[s["bias"]], a_dtype=canz.DT_MX8, out_dtype=canz.DT_BF16),
+                       canz.Linear(m=t, n=k, k=n, a=[s["dy"]], b=[s["w"]], c=[o["dx"]], b_trans=True, out_dtype=canz.DT_BF16),
+                       canz.Linear(m=n, n=k, k=t, a=[s["dy"]], b=[x8], c=[o["dw"]], a_sums=[o["db"]], a_trans=True, b_trans=True, b_dtype=canz.DT_MX8,
+                                   out_dtype=canz.DT_F32)]
+        need = max(canz.canz_linear_workspace_bytes(s["groups"][:1]), canz.canz_linear_workspace_bytes(s["groups"][1:]))
+    s["ws"] = torch.empty(max(256, need), dtype=torch.uint8, device=DEV)
+
+
+def _run_own(s):
+    canz, c = s["canz"], s["case"]
+    stream = torch.cuda.current_stream().cuda_stream
+    ws = s["ws"]
+    if c["op"] == "norm":
+        canz.canz_norm_forward(s["forward"], stream)
+        if c["mode"] == "serve":
+            canz.canz_mx8_load(s["back"], stream)
+        else:
+            if s["store"]:
+                canz.canz_mx8_store(s["store"], stream)
+            canz.canz_norm_backward(s["backward"], ws, ws.numel(), stream)
+    elif c["op"] == "gate":
+        canz.canz_act_forward(s["forward"], stream)
+        canz.canz_act_backward(s["backward"], stream)
+    elif c["op"] == "keep":
+        canz.canz_mx8_store(s["store"], stream)
+        canz.canz_mx8_load(s["back"], stream)
+    elif c["op"] == "linear":
+        canz.canz_linear(s["groups"], ws, ws.numel(), stream)
+        if s["back"]:
+            canz.canz_mx8_load(s["back"], stream)
+    else:
+        # forward, then backward
+        canz.canz_linear(s["groups"][:1], ws, ws.numel(), stream)
+        canz.canz_linear(s["groups"][1:], ws, ws.numel(), stream)
+    return s["out"]
+
+
+# ---------------------------------------------------------------- accounting and oracle
+
+def work(case):
+    size = dict(f32=4, bf16=2)
+    image = 33.0 / 32          # bytes an element: a code and its share of a scale byte
+    if case["op"] == "norm":
+        el, st = case["rows"] * case["cols"], size[case["sum"]]
+        forward = el * (2 + 2 * st + 2) + 4 * case["cols"]
+        if case["mode"] == "serve":
+            return {"bytes": forward + el * (image + image + 2), "flops": 0}
+        backward = el * (2 + 2 * st) + 8 * case["cols"]
+        return {"bytes": forward + backward + el * (st + 2 * image if case["kept"] == "8bit" else st), "flops": 0}
+    if case["op"] == "gate":
+        el, st, two = case["rows"] * case["cols"], size[case["dtype"]], 1 + case["up"]
+        return {"bytes": el * (two * (st + image) + st + st + two * (image + st) + st), "flops": 0}
+    if case["op"] == "keep":
+        return {"bytes": case["rows"] * case["cols"] * case["count"] * 2 * (size[case["dtype"]] + image), "flops": 0}
+    if case["op"] == "linear":
+        ms, n, k, out = _parts(case), case["n"], case["k"], size[case["out"]]
+        used, rows = sum(m > 0 for m in ms), sum(ms)
+        el = rows * n * (out * (1 + case["residual"]) + case["pre"] * (2 * image + 2))
+        return {"bytes": rows * k * (image if case["x"] == "8bit" else 2) + used * n * (2 * k + 4 * case["bias"]) + el, "flops": 2 * rows * n * k}
+    t, n, k = case["tokens"], case["n"], case["k"]
+    return {"bytes": t * k * image + t * n * 2 + 2 * n * k + t * n * 2 + t * k * 2 + n * k * 4 + 8 * n, "flops": 6 * t * n * k}
+
+
+def _eight64(x):
+    """As the definition says, in 64 bits, by comparison with the values and the borders between them."""
+    v = x.double()
+    rows, k = v.shape
+    pad = -k % BLOCK
+    if pad:
+        v = torch.cat([v, v.new_zeros(rows, pad)], 1)
+    v = v.reshape(rows, (k + pad) // BLOCK, BLOCK)
+    amax = v.abs().amax(2, keepdim=True)
+    unit = torch.exp2(torch.ceil(torch.log2(amax.clamp(min=2.0 ** -149) / 448)).clamp(min=-124))
+    values = [m / 8 * 2.0 ** -6 for m in range(8)] + [(1 + m / 8) * 2.0 ** e for e in range(-6, 9) for m in range(8)][:-1]
+    grid = torch.tensor(values, dtype=torch.float64, device=x.device)          # 0 .. 448
+    border = (grid[1:] + grid[:-1]) / 2
+    a = v.abs() / unit
+    code = torch.bucketize(a, border)                                          # a tie stays below
+    at = code.clamp(max=len(values) - 2)
+    code = code + ((a == border[at]) & (code < len(values) - 1) & (at % 2 == 1)).long()   # ... unless that code is odd
+    return (grid[code] * torch.sign(v) * unit).reshape(rows, k + pad)[:, :k]
+
+
+def _act64(name, z):
+    if name == "none":
+        return z, torch.ones_like(z)
+    if name == "relu":
+        return torch.where(z > 0, z, torch.zeros_like(z)), torch.where(z > 0, torch.ones_like(z), torch.zeros_like(z))
+    if name == "silu":
+        p = torch.sigmoid(z)
+        return z * p, p + z * p * torch.sigmoid(-z)
+    p = torch.special.ndtr(z)
+    return z * p, p + z * torch.exp(-z.square() / 2) / math.sqrt(2 * math.pi)
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    if case["op"] == "norm":
+        h = (s["x"].double() + s["residual"].double()).float().to(DTYPES[case["sum"]]).double()
+        var = (h * h).sum(1, keepdim=True) / case["cols"]
+        rstd = 1 / torch.sqrt(var + EPS)
+        w = s["w"].double()
+        y = w * (h * rstd)
+        if case["mode"] == "serve":
+            return dict(sum=h, y=y, y8=_eight64(y))
+        total, h = h, _eight64(h) if case["kept"] == "8bit" else h
+        u = s["dy"].double() * w
+        dx = rstd * u - rstd ** 3 * h * (u * h).sum(1, keepdim=True) / case["cols"] + s["dsum"].double()
+        return dict(sum=total, y=y, rstd=rstd[:, 0], dx=dx, dw=(s["dy"].double() * h * rstd).sum(0))
+    if case["op"] == "gate":
+        a, _ = _act64(case["act"], s["gate"].double())
+        out = a * s["up"].double() if case["up"] else a
+        a, da = _act64(case["act"], _eight64(s["gate"]))
+        dout = s["dout"].double()
+        if not case["up"]:
+            return dict(out=out, again=a, dgate=dout * da)
+        up = _eight64(s["up"])
+        return dict(out=out, again=a * up, dgate=dout * da * up, dup=dout * a)
+    if case["op"] == "keep":
+        return [_eight64(x) for x in s["x"]]
+    if case["op"] == "linear":
+        y, pre = [], []
+        for i, (x, w) in enumerate(zip(s["x"], s["w"])):
+            z = x.double() @ w.double().t()
+            z = z + s["bias"][i].double() if case["bias"] else z
+            pre.append(_eight64(z) if case["pre"] else None)
+            z = _act64(case["act"], z)[0]
+            y.append(z + s["residual"][i].double() if case["residual"] else z)
+        return dict(y=y, pre=pre if case["pre"] else [])
+    x, dy, w = s["x"].double(), s["dy"].double(), s["w"].double()
+    return dict(y=x @ w.t() + s["bias"].double(), dx=dy @ w, dw=dy.t().contiguous() @ x, db=dy.sum(0))
