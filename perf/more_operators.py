@@ -247,11 +247,11 @@ def _keep(s):
     bf16 = torch.bfloat16
 
     def image(rows, cols):
-        return torch.empty(max(256, canz.canz_mx8_bytes(rows, cols)), dtype=torch.uint8, device=DEV)
+        return torch.empty(max(256, canz.canz_mx_eight_bytes(rows, cols)), dtype=torch.uint8, device=DEV)
 
     def stored(x):
         im = image(*x.shape)
-        canz.canz_mx8_store([canz.Mx8Group(rows=x.shape[0], cols=x.shape[1], mat=[x], image=[im], dtype=canz.DT_BF16)], stream)
+        canz.canz_mx_eight_store([canz.Mx8Group(rows=x.shape[0], cols=x.shape[1], mat=[x], image=[im], dtype=canz.DT_BF16)], stream)
         return im
 
     def empty(rows, cols, dtype):
@@ -322,21 +322,21 @@ def _run_own(s):
     if c["op"] == "norm":
         canz.canz_norm_forward(s["forward"], stream)
         if c["mode"] == "serve":
-            canz.canz_mx8_load(s["back"], stream)
+            canz.canz_mx_eight_load(s["back"], stream)
         else:
             if s["store"]:
-                canz.canz_mx8_store(s["store"], stream)
+                canz.canz_mx_eight_store(s["store"], stream)
             canz.canz_norm_backward(s["backward"], ws, ws.numel(), stream)
     elif c["op"] == "gate":
         canz.canz_act_forward(s["forward"], stream)
         canz.canz_act_backward(s["backward"], stream)
     elif c["op"] == "keep":
-        canz.canz_mx8_store(s["store"], stream)
-        canz.canz_mx8_load(s["back"], stream)
+        canz.canz_mx_eight_store(s["store"], stream)
+        canz.canz_mx_eight_load(s["back"], stream)
     elif c["op"] == "linear":
         canz.canz_linear(s["groups"], ws, ws.numel(), stream)
         if s["back"]:
-            canz.canz_mx8_load(s["back"], stream)
+            canz.canz_mx_eight_load(s["back"], stream)
     else:
         # forward, then backward
         canz.canz_linear(s["groups"][:1], ws, ws.numel(), stream)
