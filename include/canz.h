@@ -41,7 +41,8 @@ enum {
 
 enum { CANZ_COST_NUMEL = 0, CANZ_COST_NS_FLOPS = 1, CANZ_COST_SHAMPOO_FLOPS = 2, CANZ_COST_SOAP_FLOPS = 3 };
 #define CANZ_SOAP_COST_MAX_PRECOND_DIM 10000 /* the limit CANZ_COST_SOAP_FLOPS assumes for canz_soap_hparams.max_precond_dim */
-enum { CANZ_DT_F32 = 0, CANZ_DT_BF16 = 1, CANZ_DT_MX = 2 /* a microscaled image: a_dtype of canz_mx_product only */ };
+enum { CANZ_DT_F32 = 0, CANZ_DT_BF16 = 1, CANZ_DT_MX = 2 /* a microscaled image: a_dtype of canz_mx_product only */,
+       CANZ_DT_MX8 = 3 /* an 8-bit image (canz_mx_eight_store), where a call says so */ };
 enum { CANZ_SCALE_NONE = 0, CANZ_SCALE_ASPECT = 1, CANZ_SCALE_RMS = 2 };
 enum { CANZ_PREC_BF16 = 0, CANZ_PREC_F32 = 1 };
 enum { CANZ_OUT_PARAM = 0, CANZ_OUT_DELTA = 1 };
@@ -565,6 +566,151 @@ int canz_muon_step_images(const canz_group* g, int32_t n_groups, const canz_muon
                           void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /*
+ * What lies around the matrices of a step in training and serving: the norm in front of a linear layer, the layer's products in bf16,
+ * the activation behind it, and 8-bit images in which activations wait for the backward pass.  One half of a block, forward
+ *   h = x + residual, y = norm(h)        canz_norm_forward      y as bf16 and as an 8-bit image that is operand and checkpoint
+ *   z = y W^T + bias, a = act(z)         canz_linear            z kept in 8 bits
+ *   or a = act(gate) up                  canz_act_forward       gate and up kept in 8 bits
+ *   out = a W2^T + residual              canz_linear
+ * and backward
+ *   da = dout W2, dW2 = dout^T a         canz_linear            a restored from its arguments' images
+ *   dz = da act'(z)                      canz_act_backward
+ *   dy = dz W, dW = dz^T y, dbias        canz_linear            y from its image; dW is the gradient that enters a step
+ *   dx = ..., dw                         canz_norm_backward
+ *
+ * Conventions of all these calls.  Matrices are row-major in fp32 or bf16, at any address that is a multiple of their element's size; rows lie any number of elements
+ * apart, at least their length, and what lies between them stays as it is.  8-bit images and workspaces are 256-byte aligned.  Extents are at
+ * most 4194240 each, padded matrices (images: see below) at most 2^37 elements; an extent may be 0.  Tables and structures are the host's and are read
+ * during the call.  The calls issue kernel launches only (no allocation, copy, memset or synchronisation), on the device hip_stream
+ * belongs to (NULL, hipStreamLegacy and hipStreamPerThread: the current one), and may be recorded into a HIP graph.  What a call writes must not overlap any other buffer of
+ * the call, but where it says so; what it only reads may be given any number of times.  Sums are formed in fp32 in an order that depends on extents
+ * alone, an element is rounded once to the type of its matrix, and results do not depend on what else is in the call.  Infinities and NaN go through
+ * the formulas as fp32 arithmetic has it.
+ * Errors of all of them: CANZ_EINVAL (null pointers that are needed, misaligned ones, negative extents or counts, a row distance below the row's length), CANZ_ESHAPE
+ * (an extent or a matrix above the limits), CANZ_EUNSUPPORTED (enums), CANZ_EWORKSPACE (missing, misaligned or too small), all before anything is
+ * enqueued; CANZ_EHIP (earlier entries may be enqueued already).
+ *
+ * An 8-bit image (MXFP8) of a matrix: every 32 consecutive elements of a row (the last ones may be fewer) are a block with a common X, a power of two in an
+ * E8M0 byte (2^(byte - 127)): the smallest one with amax <= 448 X for the largest magnitude amax of the block, within 2^-124 .. 2^119.  An element is held in a byte
+ * (E4M3: a sign, 4 significant bits down to 2^-6, the spacing 2^-9 below, at most 448) as the value nearest to it, ties to the even code, times X: off by
+ * at most 2^-4 of itself or 2^-10 X (magnitudes above 448 2^119 = 2.98e38 become that).  Every value is finite and exact in fp32 and in bf16.  A block that holds an infinity or a NaN is NaN as a
+ * whole (byte 255, codes 0).  In memory: the codes row by row, rows padded to multiples of 128 bytes, then the scale bytes row by row, a
+ * 32nd of that; padding is written as zeros with scale 0 and not looked at.  Images may be copied and sent as canz_mx_eight_bytes() bytes.
+ */
+
+/* Bytes of an 8-bit image of `rows` x `cols` elements (a multiple of 256; 0 if an extent is 0). */
+int canz_mx_eight_bytes(int64_t rows, int64_t cols, size_t* bytes_out);
+
+/* Matrices of one shape and type with their 8-bit images. */
+typedef struct {
+  int64_t rows, cols;
+  int64_t ld;                /* elements from a row of mat to the next, >= cols */
+  int32_t n_mats;
+  int32_t dtype;             /* of mat: CANZ_DT_F32 or CANZ_DT_BF16            */
+  void* const* mat;          /* [n_mats]                                        */
+  void* const* image;        /* [n_mats]                                        */
+} canz_mx8_group;
+
+/* canz_mx_eight_store - enqueue the 8-bit images of the given matrices; canz_mx_eight_load - the values they stand for, back into mat. */
+int canz_mx_eight_store(const canz_mx8_group* g, int32_t n_groups, void* hip_stream);
+int canz_mx_eight_load(const canz_mx8_group* g, int32_t n_groups, void* hip_stream);
+
+/*
+ * Activations.  CANZ_ACT_SILU z / (1 + e^-z), CANZ_ACT_GELU z Phi(z) with the normal distribution's Phi, CANZ_ACT_RELU max(z, 0) (with slope 0 at 0; a NaN stays one).
+ */
+enum { CANZ_ACT_NONE = 0, CANZ_ACT_SILU = 1, CANZ_ACT_GELU = 2, CANZ_ACT_RELU = 3 };
+
+/* out = act(gate) up, or act(gate) where up is NULL. */
+typedef struct {
+  int64_t rows, cols;
+  int64_t ld_in;             /* rows of gate and up (the halves of one matrix, for instance) */
+  int64_t ld_out;            /* rows of out                                                  */
+  int32_t act;               /* CANZ_ACT_*                                                   */
+  int32_t dtype;             /* of gate, up and out: CANZ_DT_F32 or CANZ_DT_BF16             */
+  const void* gate;
+  const void* up;            /* or NULL                                                      */
+  void* out;                 /* or NULL                                                      */
+  void* gate8;               /* 8-bit image of gate for the backward pass, or NULL           */
+  void* up8;                 /* of up, or NULL                                               */
+} canz_act;
+
+/* canz_act_forward - enqueue a[0 .. n).  CANZ_EINVAL as well if nothing is asked for, or up8 without up. */
+int canz_act_forward(const canz_act* a, int32_t n, void* hip_stream);
+
+/* dgate = dout up act'(gate), dup = dout act(gate), and out = act(gate) up once more; without up as if it were 1. */
+typedef struct {
+  int64_t rows, cols;
+  int64_t ld_in;             /* rows of gate, up (matrices), dgate and dup                   */
+  int64_t ld_out;            /* rows of dout and out                                         */
+  int32_t act;
+  int32_t dtype;             /* of dout, dgate, dup and out                                  */
+  int32_t in_dtype;          /* of gate and up: CANZ_DT_F32, CANZ_DT_BF16 or CANZ_DT_MX8     */
+  const void* dout;          /* may be NULL where only out is asked for                      */
+  const void* gate;
+  const void* up;            /* or NULL                                                      */
+  void* dgate;               /* or NULL; may be gate itself (matrices of one type)           */
+  void* dup;                 /* or NULL; may be up itself                                    */
+  void* out;                 /* or NULL; may be dout itself                                  */
+} canz_act_grad;
+
+/* canz_act_backward - enqueue a[0 .. n).  CANZ_EINVAL as well if nothing is asked for, or dup without up. */
+int canz_act_backward(const canz_act_grad* a, int32_t n, void* hip_stream);
+
+/*
+ * The root-mean-square norm with the residual's addition.  h = x + residual (x where residual is NULL), rounded to sum_dtype; per row of h
+ *   rstd = 1 / sqrt(mean(h^2) + eps),  y = weight h rstd
+ * h is what goes on as the residual stream; the norm is that of the rounded h whether sum is asked for or not.
+ */
+typedef struct {
+  int64_t rows, cols;
+  int64_t ldx;               /* rows of x                                                    */
+  int64_t lds;               /* rows of residual and sum                                     */
+  int64_t ldy;               /* rows of y                                                    */
+  int32_t dtype;             /* of x and y: CANZ_DT_F32 or CANZ_DT_BF16                      */
+  int32_t sum_dtype;         /* of residual and sum                                          */
+  int32_t weight_dtype;
+  float eps;                 /* >= 0                                                         */
+  const void* x;
+  const void* residual;      /* or NULL                                                      */
+  const void* weight;        /* [cols]                                                       */
+  void* sum;                 /* h, or NULL; may be residual itself                           */
+  void* y;                   /* or NULL                                                      */
+  void* y8;                  /* 8-bit image of y before its rounding to dtype, or NULL       */
+  float* rstd;               /* [rows] for the backward pass, or NULL                        */
+} canz_norm;
+
+/* canz_norm_forward - enqueue a[0 .. n).  CANZ_EINVAL as well if nothing is asked for, or eps is negative or NaN. */
+int canz_norm_forward(const canz_norm* a, int32_t n, void* hip_stream);
+
+/*
+ * Its gradients, with u = weight dy, n = h rstd and the mean over a row:
+ *   dx = dsum + rstd (u - n mean(u n)),  for x and residual alike;  dweight <- beta dweight + sum over the rows of dy n
+ * (dweight is not read where beta is 0).
+ */
+typedef struct {
+  int64_t rows, cols;
+  int64_t ldy;               /* rows of dy                                                   */
+  int64_t lds;               /* rows of h (a matrix), dsum and dx                            */
+  int32_t dtype;             /* of dy                                                        */
+  int32_t sum_dtype;         /* of dsum and dx                                               */
+  int32_t h_dtype;           /* CANZ_DT_F32, CANZ_DT_BF16 or CANZ_DT_MX8 (an image of h)     */
+  int32_t weight_dtype;
+  float beta;
+  const void* dy;
+  const void* h;
+  const float* rstd;         /* [rows], of the forward pass                                  */
+  const void* weight;        /* [cols]                                                       */
+  const void* dsum;          /* gradient that reaches h along the residual stream, or NULL   */
+  void* dx;                  /* or NULL; may be dsum itself                                  */
+  float* dweight;            /* [cols] fp32, or NULL                                         */
+} canz_norm_grad;
+
+/* Device scratch canz_norm_backward needs (at least 256; shared by the entries, which run one after another).  Pointers: only dweight's being NULL counts. */
+int canz_norm_backward_workspace_bytes(const canz_norm_grad* a, int32_t n, size_t* bytes_out);
+/* canz_norm_backward - enqueue a[0 .. n).  CANZ_EINVAL as well if neither dx nor dweight is asked for. */
+int canz_norm_backward(const canz_norm_grad* a, int32_t n, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
  * Per-kernel timing of canz_muon_step / canz_shampoo_step / canz_soap_step, for benchmarks (the measurement protocol of
  * App. C.1 reports the optimizer time; this splits it by kernel).  While enabled, every
  * kernel launch of a step is bracketed by a pair of HIP events on the step's own stream.
@@ -577,7 +723,7 @@ int canz_muon_step_images(const canz_group* g, int32_t n_groups, const canz_muon
  *                         launch counts per kernel kind into ms_out / launches_out
  *                         (host arrays of CANZ_KERNEL_KINDS entries) and starts a new period.
  *   canz_profile_disable  stops recording.
- * The launches of canz_mx_* are not recorded.
+ * The launches of canz_mx_*, canz_mx_eight_*, canz_act_*, canz_norm_* and canz_linear are not recorded.
  */
 enum {
   CANZ_KERNEL_MOMENTUM = 0, /* momentum + gather + cast + norm partial sums */

@@ -22,17 +22,20 @@ LIB_PATH = os.path.join(_HERE, "libcanz.so")
 
 OK, EINVAL, ESHAPE, EWORKSPACE, EHIP, EUNSUPPORTED = 0, -1, -2, -3, -4, -5
 COST_NUMEL, COST_NS_FLOPS, COST_SHAMPOO_FLOPS, COST_SOAP_FLOPS = 0, 1, 2, 3
-DT_F32, DT_BF16, DT_MX = 0, 1, 2
+DT_F32, DT_BF16, DT_MX, DT_MX8 = 0, 1, 2, 3
 SCALE_NONE, SCALE_ASPECT, SCALE_RMS = 0, 1, 2
 PREC_BF16, PREC_F32 = 0, 1
 OUT_PARAM, OUT_DELTA = 0, 1
 MX_SCALE_FLOOR, MX_SCALE_CEIL = 0, 1
+ACT_NONE, ACT_SILU, ACT_GELU, ACT_RELU = 0, 1, 2, 3
 
 EXPORTS = ("canz_last_error", "canz_version", "canz_partition_alpha", "canz_partition_naive", "canz_microgroup_plan", "canz_tp_schedule",
            "canz_muon_workspace_bytes", "canz_muon_step", "canz_muon_step_static",
            "canz_shampoo_workspace_bytes", "canz_shampoo_step", "canz_soap_workspace_bytes", "canz_soap_step",
            "canz_mx_image_bytes", "canz_mx_quantize", "canz_mx_dequantize", "canz_mx_product_workspace_bytes", "canz_mx_product",
            "canz_muon_step_images",
+           "canz_mx_eight_bytes", "canz_mx_eight_store", "canz_mx_eight_load", "canz_act_forward", "canz_act_backward",
+           "canz_norm_forward", "canz_norm_backward_workspace_bytes", "canz_norm_backward",
            "canz_profile_enable", "canz_profile_collect", "canz_profile_disable")
 KERNEL_KINDS = ("momentum", "norm", "gram", "poly", "update", "final", "apply",
                 "sh_load", "sh_stat", "sh_init", "sh_root", "sh_apply",
@@ -103,6 +106,34 @@ class _MxImages(C.Structure):
     _fields_ = [("by_row", C.POINTER(C.c_void_p)), ("by_col", C.POINTER(C.c_void_p))]
 
 
+class _Mx8Group(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("ld", C.c_int64), ("n_mats", C.c_int32), ("dtype", C.c_int32),
+                ("mat", C.POINTER(C.c_void_p)), ("image", C.POINTER(C.c_void_p))]
+
+
+class _Act(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("ld_in", C.c_int64), ("ld_out", C.c_int64), ("act", C.c_int32), ("dtype", C.c_int32),
+                ("gate", C.c_void_p), ("up", C.c_void_p), ("out", C.c_void_p), ("gate8", C.c_void_p), ("up8", C.c_void_p)]
+
+
+class _ActGrad(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("ld_in", C.c_int64), ("ld_out", C.c_int64), ("act", C.c_int32), ("dtype", C.c_int32),
+                ("in_dtype", C.c_int32), ("dout", C.c_void_p), ("gate", C.c_void_p), ("up", C.c_void_p), ("dgate", C.c_void_p), ("dup", C.c_void_p),
+                ("out", C.c_void_p)]
+
+
+class _Norm(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("ldx", C.c_int64), ("lds", C.c_int64), ("ldy", C.c_int64), ("dtype", C.c_int32),
+                ("sum_dtype", C.c_int32), ("weight_dtype", C.c_int32), ("eps", C.c_float), ("x", C.c_void_p), ("residual", C.c_void_p),
+                ("weight", C.c_void_p), ("sum", C.c_void_p), ("y", C.c_void_p), ("y8", C.c_void_p), ("rstd", C.c_void_p)]
+
+
+class _NormGrad(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("ldy", C.c_int64), ("lds", C.c_int64), ("dtype", C.c_int32), ("sum_dtype", C.c_int32),
+                ("h_dtype", C.c_int32), ("weight_dtype", C.c_int32), ("beta", C.c_float), ("dy", C.c_void_p), ("h", C.c_void_p), ("rstd", C.c_void_p),
+                ("weight", C.c_void_p), ("dsum", C.c_void_p), ("dx", C.c_void_p), ("dweight", C.c_void_p)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise RuntimeError("libcanz.so is missing at %s - build it with "
@@ -161,6 +192,15 @@ def _load():
     lib.canz_muon_step_images.argtypes = [C.POINTER(_Group), C.c_int32, C.POINTER(_Hparams), C.POINTER(_MxImages), C.c_int32,
                                           C.c_void_p, C.c_size_t, C.c_void_p]
     lib.canz_muon_step_images.restype = C.c_int
+    lib.canz_mx_eight_bytes.argtypes = [C.c_int64, C.c_int64, C.POINTER(C.c_size_t)]
+    lib.canz_mx_eight_bytes.restype = C.c_int
+    for name in ("canz_mx_eight_store", "canz_mx_eight_load", "canz_act_forward", "canz_act_backward", "canz_norm_forward"):
+        getattr(lib, name).argtypes = [C.c_void_p, C.c_int32, C.c_void_p]
+        getattr(lib, name).restype = C.c_int
+    lib.canz_norm_backward_workspace_bytes.argtypes = [C.c_void_p, C.c_int32, C.POINTER(C.c_size_t)]
+    lib.canz_norm_backward_workspace_bytes.restype = C.c_int
+    lib.canz_norm_backward.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.canz_norm_backward.restype = C.c_int
     lib.canz_profile_enable.argtypes = [C.c_int32]
     lib.canz_profile_enable.restype = C.c_int
     lib.canz_profile_collect.argtypes = [C.POINTER(C.c_double), i64p]
@@ -590,6 +630,177 @@ def canz_muon_step_images(groups: Sequence[Group], hp: Hparams, images: Sequence
     h = hp._c()
     _check(_lib.canz_muon_step_images(arr, len(groups), C.byref(h), im, int(scale_mode), C.c_void_p(_addr(workspace)),
                                       int(workspace_bytes), C.c_void_p(int(stream))))
+
+
+def canz_mx_eight_bytes(rows: int, cols: int) -> int:
+    """Bytes of an 8-bit image of ``rows`` x ``cols`` elements."""
+    out = C.c_size_t(0)
+    _check(_lib.canz_mx_eight_bytes(int(rows), int(cols), C.byref(out)))
+    return int(out.value)
+
+
+@dataclass
+class Mx8Group:
+    """Matrices of one shape and their 8-bit images: device buffers given as addresses or objects with data_ptr()."""
+    rows: int
+    cols: int
+    mat: Sequence = field(default_factory=list)      # n_mats
+    image: Sequence = field(default_factory=list)    # n_mats
+    dtype: int = DT_BF16
+    ld: int = -1                                     # -1: cols
+    n_mats: int = -1                                 # -1: len(mat)
+
+
+@dataclass
+class Act:
+    """out = act(gate) up, or act(gate) without up; gate8 and up8 receive 8-bit images of the arguments."""
+    rows: int
+    cols: int
+    gate: object = None
+    up: object = None
+    out: object = None
+    gate8: object = None
+    up8: object = None
+    act: int = ACT_SILU
+    dtype: int = DT_BF16
+    ld_in: int = -1                                  # rows of gate and up; -1: cols
+    ld_out: int = -1                                 # rows of out; -1: cols
+
+
+@dataclass
+class ActGrad:
+    """dgate, dup and out once more, from gate and up as matrices or as 8-bit images (in_dtype)."""
+    rows: int
+    cols: int
+    dout: object = None
+    gate: object = None
+    up: object = None
+    dgate: object = None
+    dup: object = None
+    out: object = None
+    act: int = ACT_SILU
+    dtype: int = DT_BF16
+    in_dtype: int = DT_MX8
+    ld_in: int = -1                                  # rows of gate and up (matrices), dgate and dup; -1: cols
+    ld_out: int = -1                                 # rows of dout and out; -1: cols
+
+
+@dataclass
+class Norm:
+    """h = x + residual (sum), y = weight h rstd with rstd = 1 / sqrt(mean(h^2) + eps); y8 receives an 8-bit image of y."""
+    rows: int
+    cols: int
+    x: object = None
+    weight: object = None
+    y: object = None
+    y8: object = None
+    residual: object = None
+    sum: object = None
+    rstd: object = None
+    dtype: int = DT_BF16
+    sum_dtype: int = -1                              # of residual and sum; -1: dtype
+    weight_dtype: int = DT_F32
+    eps: float = 1e-6
+    ldx: int = -1                                    # rows of x; -1: cols
+    lds: int = -1                                    # rows of residual and sum; -1: cols
+    ldy: int = -1                                    # rows of y; -1: cols
+
+
+@dataclass
+class NormGrad:
+    """Gradients of Norm: dx (for x and residual) and dweight <- beta dweight + ..., from h as a matrix or as an 8-bit image (h_dtype)."""
+    rows: int
+    cols: int
+    dy: object = None
+    h: object = None
+    rstd: object = None
+    weight: object = None
+    dx: object = None
+    dsum: object = None
+    dweight: object = None
+    dtype: int = DT_BF16                             # of dy
+    sum_dtype: int = -1                              # of dsum and dx; -1: dtype
+    h_dtype: int = -1                                # -1: sum_dtype
+    weight_dtype: int = DT_F32
+    beta: float = 0.0
+    ldy: int = -1                                    # rows of dy; -1: cols
+    lds: int = -1                                    # rows of h (a matrix), dsum and dx; -1: cols
+
+
+_MX8_GROUP = struct.Struct("@3q2i2P")
+_ACT = struct.Struct("@4q2i5P")
+_ACT_GRAD = struct.Struct("@4q3i4x6P")
+_NORM = struct.Struct("@5q3if7P")
+_NORM_GRAD = struct.Struct("@4q4if4x7P")
+assert all(x.size == C.sizeof(y) for x, y in ((_MX8_GROUP, _Mx8Group), (_ACT, _Act), (_ACT_GRAD, _ActGrad), (_NORM, _Norm), (_NORM_GRAD, _NormGrad)))
+
+
+def _at(x) -> int:
+    """Device address of a buffer, or 0 for None."""
+    return x.data_ptr() if hasattr(x, "data_ptr") else x or 0
+
+
+def _marshal_mx8(groups: Sequence[Mx8Group]):
+    keep, packed = [], []
+    for g in groups:
+        n = len(g.mat) if g.n_mats == -1 else g.n_mats
+        packed.append(_MX8_GROUP.pack(g.rows, g.cols, g.cols if g.ld == -1 else g.ld, n, g.dtype, _table(g.mat, keep, n), _table(g.image, keep, n)))
+    return b"".join(packed), keep
+
+
+def canz_mx_eight_store(groups: Sequence[Mx8Group], stream=0) -> None:
+    """Enqueue the 8-bit images of the given matrices on ``stream``."""
+    arr, _keep = _marshal_mx8(groups)
+    _check(_lib.canz_mx_eight_store(arr, len(groups), stream))
+
+
+def canz_mx_eight_load(groups: Sequence[Mx8Group], stream=0) -> None:
+    """Enqueue the values that the given 8-bit images stand for, into mat."""
+    arr, _keep = _marshal_mx8(groups)
+    _check(_lib.canz_mx_eight_load(arr, len(groups), stream))
+
+
+def canz_act_forward(acts: Sequence[Act], stream=0) -> None:
+    """Enqueue the given activations on ``stream``."""
+    arr = b"".join([_ACT.pack(a.rows, a.cols, a.cols if a.ld_in == -1 else a.ld_in, a.cols if a.ld_out == -1 else a.ld_out, a.act, a.dtype,
+                              _at(a.gate), _at(a.up), _at(a.out), _at(a.gate8), _at(a.up8)) for a in acts])
+    _check(_lib.canz_act_forward(arr, len(acts), stream))
+
+
+def canz_act_backward(acts: Sequence[ActGrad], stream=0) -> None:
+    """Enqueue the gradients of the given activations on ``stream``."""
+    arr = b"".join([_ACT_GRAD.pack(a.rows, a.cols, a.cols if a.ld_in == -1 else a.ld_in, a.cols if a.ld_out == -1 else a.ld_out, a.act, a.dtype,
+                                   a.in_dtype, _at(a.dout), _at(a.gate), _at(a.up), _at(a.dgate), _at(a.dup), _at(a.out)) for a in acts])
+    _check(_lib.canz_act_backward(arr, len(acts), stream))
+
+
+def canz_norm_forward(norms: Sequence[Norm], stream=0) -> None:
+    """Enqueue the given norms on ``stream``."""
+    arr = b"".join([_NORM.pack(a.rows, a.cols, *[a.cols if d == -1 else d for d in (a.ldx, a.lds, a.ldy)], a.dtype,
+                               a.dtype if a.sum_dtype == -1 else a.sum_dtype, a.weight_dtype, a.eps, _at(a.x), _at(a.residual), _at(a.weight),
+                               _at(a.sum), _at(a.y), _at(a.y8), _at(a.rstd)) for a in norms])
+    _check(_lib.canz_norm_forward(arr, len(norms), stream))
+
+
+def _marshal_norm_grad(norms: Sequence[NormGrad]) -> bytes:
+    packed = []
+    for a in norms:
+        sum_dtype = a.dtype if a.sum_dtype == -1 else a.sum_dtype
+        packed.append(_NORM_GRAD.pack(a.rows, a.cols, a.cols if a.ldy == -1 else a.ldy, a.cols if a.lds == -1 else a.lds, a.dtype, sum_dtype,
+                                      sum_dtype if a.h_dtype == -1 else a.h_dtype, a.weight_dtype, a.beta, _at(a.dy), _at(a.h), _at(a.rstd),
+                                      _at(a.weight), _at(a.dsum), _at(a.dx), _at(a.dweight)))
+    return b"".join(packed)
+
+
+def canz_norm_backward_workspace_bytes(norms: Sequence[NormGrad]) -> int:
+    out = C.c_size_t(0)
+    _check(_lib.canz_norm_backward_workspace_bytes(_marshal_norm_grad(norms), len(norms), C.byref(out)))
+    return int(out.value)
+
+
+def canz_norm_backward(norms: Sequence[NormGrad], workspace, workspace_bytes: int, stream=0) -> None:
+    """Enqueue the gradients of the given norms on ``stream``."""
+    _check(_lib.canz_norm_backward(_marshal_norm_grad(norms), len(norms), _at(workspace), workspace_bytes, stream))
 
 
 def canz_profile_enable(max_launches: int) -> None:
