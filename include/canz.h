@@ -711,6 +711,51 @@ int canz_norm_backward_workspace_bytes(const canz_norm_grad* a, int32_t n, size_
 int canz_norm_backward(const canz_norm_grad* a, int32_t n, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /*
+ * Products of one shape with everything a linear layer does to their results:
+ *   z = alpha A B^T + bias,  C = act(z) + beta R
+ * A is m x k, or stored k x m with a_trans; B is n x k, or stored k x n with b_trans; each in bf16 or as an 8-bit image of the stored matrix.  R is the residual, or C
+ * itself where there is none (gradients added up over several calls); it is not read where beta is 0.  z leaves as an 8-bit image, too, where pre8 asks for it, and the
+ * rows of A are summed: a_sums <- alpha sum over k of A + beta a_sums (a bias' gradient where A^T is that of the layer's output; not read where beta is 0).
+ *   y = x W^T + bias         A = x (tokens x in)                  B = W (out x in)
+ *   dx = dy W                A = dy (tokens x out)                B = W, b_trans
+ *   dW = dy^T x, dbias       A = dy, a_trans                      B = x, b_trans
+ * Products of two elements are exact, sums over k in fp32.
+ */
+typedef struct {
+  int64_t m, n, k;
+  int64_t lda, ldb;          /* elements from a stored row of A, B to the next; not looked at for images */
+  int64_t ldc, ldr;          /* of C, of the residual (not looked at without one)                        */
+  int32_t n_prods;
+  int32_t a_dtype, b_dtype;  /* CANZ_DT_BF16 or CANZ_DT_MX8                                              */
+  int32_t out_dtype;         /* of C and the residual: CANZ_DT_F32 or CANZ_DT_BF16                       */
+  int32_t bias_dtype;        /* CANZ_DT_F32 or CANZ_DT_BF16                                              */
+  int32_t a_trans, b_trans;  /* 0 or 1                                                                   */
+  int32_t act;               /* CANZ_ACT_*                                                               */
+  float alpha, beta;
+  const void* const* a;      /* [n_prods]                                                                */
+  const void* const* b;      /* [n_prods]                                                                */
+  const void* const* bias;   /* [n_prods] of n elements, or NULL                                         */
+  const void* const* residual; /* [n_prods] m x n, or NULL; may be C itself, with ldr = ldc              */
+  void* const* c;            /* [n_prods] m x n                                                          */
+  void* const* pre8;         /* [n_prods] 8-bit images of m x n, or NULL                                 */
+  void* const* a_sums;       /* [n_prods] of m fp32 sums, or NULL                                        */
+} canz_linear_group;
+
+/*
+ * Device scratch canz_linear needs for these groups (at least 256).  Operands that the kernels cannot take where they lie (8-bit images; matrices that are not 16-byte aligned or whose rows'
+ * lengths or distances are no multiples of 8) are copied into it, but for the matrices of a product of up to 64 rows without a_trans and b_trans; so the addresses in a and b count,
+ * and where these tables are NULL, the worst is assumed.  Of the other tables only a_sums' being NULL counts.
+ */
+int canz_linear_workspace_bytes(const canz_linear_group* g, int32_t n_groups, size_t* bytes_out);
+
+/*
+ * canz_linear - enqueue the given products; groups may differ in every extent (experts with the rows a router gave them), and all products of a call may
+ * run at once.  The workspace is scratch that need not be initialised, and is not to be shared by calls that may run at the same time (two streams, two graphs).
+ * CANZ_ESHAPE as well if the workspace had more than 2^64 bytes.
+ */
+int canz_linear(const canz_linear_group* g, int32_t n_groups, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
  * Per-kernel timing of canz_muon_step / canz_shampoo_step / canz_soap_step, for benchmarks (the measurement protocol of
  * App. C.1 reports the optimizer time; this splits it by kernel).  While enabled, every
  * kernel launch of a step is bracketed by a pair of HIP events on the step's own stream.

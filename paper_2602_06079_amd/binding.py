@@ -36,6 +36,7 @@ EXPORTS = ("canz_last_error", "canz_version", "canz_partition_alpha", "canz_part
            "canz_muon_step_images",
            "canz_mx_eight_bytes", "canz_mx_eight_store", "canz_mx_eight_load", "canz_act_forward", "canz_act_backward",
            "canz_norm_forward", "canz_norm_backward_workspace_bytes", "canz_norm_backward",
+           "canz_linear_workspace_bytes", "canz_linear",
            "canz_profile_enable", "canz_profile_collect", "canz_profile_disable")
 KERNEL_KINDS = ("momentum", "norm", "gram", "poly", "update", "final", "apply",
                 "sh_load", "sh_stat", "sh_init", "sh_root", "sh_apply",
@@ -134,6 +135,13 @@ class _NormGrad(C.Structure):
                 ("weight", C.c_void_p), ("dsum", C.c_void_p), ("dx", C.c_void_p), ("dweight", C.c_void_p)]
 
 
+class _Linear(C.Structure):
+    _fields_ = [("m", C.c_int64), ("n", C.c_int64), ("k", C.c_int64), ("lda", C.c_int64), ("ldb", C.c_int64), ("ldc", C.c_int64), ("ldr", C.c_int64),
+                ("n_prods", C.c_int32), ("a_dtype", C.c_int32), ("b_dtype", C.c_int32), ("out_dtype", C.c_int32), ("bias_dtype", C.c_int32),
+                ("a_trans", C.c_int32), ("b_trans", C.c_int32), ("act", C.c_int32), ("alpha", C.c_float), ("beta", C.c_float)] + \
+               [(name, C.POINTER(C.c_void_p)) for name in ("a", "b", "bias", "residual", "c", "pre8", "a_sums")]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise RuntimeError("libcanz.so is missing at %s - build it with "
@@ -201,6 +209,10 @@ def _load():
     lib.canz_norm_backward_workspace_bytes.restype = C.c_int
     lib.canz_norm_backward.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]
     lib.canz_norm_backward.restype = C.c_int
+    lib.canz_linear_workspace_bytes.argtypes = [C.c_void_p, C.c_int32, C.POINTER(C.c_size_t)]
+    lib.canz_linear_workspace_bytes.restype = C.c_int
+    lib.canz_linear.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.canz_linear.restype = C.c_int
     lib.canz_profile_enable.argtypes = [C.c_int32]
     lib.canz_profile_enable.restype = C.c_int
     lib.canz_profile_collect.argtypes = [C.POINTER(C.c_double), i64p]
@@ -727,12 +739,43 @@ class NormGrad:
     lds: int = -1                                    # rows of h (a matrix), dsum and dx; -1: cols
 
 
+@dataclass
+class Linear:
+    """Products of one shape, z = alpha A B^T + bias and C = act(z) + beta R: device buffers given as addresses or objects with data_ptr()."""
+    m: int
+    n: int
+    k: int
+    a: Sequence = field(default_factory=list)        # n_prods, m x k, or k x m (a_trans)
+    b: Sequence = field(default_factory=list)        # n_prods, n x k, or k x n (b_trans)
+    c: Sequence = field(default_factory=list)        # n_prods, m x n
+    bias: Sequence = field(default_factory=list)     # n_prods of n elements, or empty
+    residual: Sequence = field(default_factory=list) # n_prods, m x n, R; empty: R is C
+    pre8: Sequence = field(default_factory=list)     # n_prods 8-bit images that receive z, or empty
+    a_sums: Sequence = field(default_factory=list)   # n_prods of m fp32 sums of A's rows, or empty
+    a_dtype: int = DT_BF16
+    b_dtype: int = DT_BF16
+    out_dtype: int = DT_BF16                         # of C and R
+    bias_dtype: int = DT_F32
+    a_trans: bool = False
+    b_trans: bool = False
+    act: int = ACT_NONE
+    alpha: float = 1.0
+    beta: float = 0.0
+    lda: int = -1                                    # -1: as long as a stored row
+    ldb: int = -1
+    ldc: int = -1
+    ldr: int = -1
+    n_prods: int = -1                                # -1: len(c)
+
+
 _MX8_GROUP = struct.Struct("@3q2i2P")
+_LINEAR = struct.Struct("@7q8i2f7P")
 _ACT = struct.Struct("@4q2i5P")
 _ACT_GRAD = struct.Struct("@4q3i4x6P")
 _NORM = struct.Struct("@5q3if7P")
 _NORM_GRAD = struct.Struct("@4q4if4x7P")
-assert all(x.size == C.sizeof(y) for x, y in ((_MX8_GROUP, _Mx8Group), (_ACT, _Act), (_ACT_GRAD, _ActGrad), (_NORM, _Norm), (_NORM_GRAD, _NormGrad)))
+assert all(x.size == C.sizeof(y) for x, y in ((_MX8_GROUP, _Mx8Group), (_ACT, _Act), (_ACT_GRAD, _ActGrad), (_NORM, _Norm), (_NORM_GRAD, _NormGrad),
+                                                        (_LINEAR, _Linear)))
 
 
 def _at(x) -> int:
@@ -801,6 +844,30 @@ def canz_norm_backward_workspace_bytes(norms: Sequence[NormGrad]) -> int:
 def canz_norm_backward(norms: Sequence[NormGrad], workspace, workspace_bytes: int, stream=0) -> None:
     """Enqueue the gradients of the given norms on ``stream``."""
     _check(_lib.canz_norm_backward(_marshal_norm_grad(norms), len(norms), _at(workspace), workspace_bytes, stream))
+
+
+def _marshal_linear(groups: Sequence[Linear]):
+    keep, packed = [], []
+    for g in groups:
+        n = len(g.c) if g.n_prods == -1 else g.n_prods
+        lda, ldb = g.m if g.a_trans else g.k, g.n if g.b_trans else g.k
+        packed.append(_LINEAR.pack(g.m, g.n, g.k, lda if g.lda == -1 else g.lda, ldb if g.ldb == -1 else g.ldb, g.n if g.ldc == -1 else g.ldc,
+                                   g.n if g.ldr == -1 else g.ldr, n, g.a_dtype, g.b_dtype, g.out_dtype, g.bias_dtype, int(g.a_trans), int(g.b_trans), g.act,
+                                   g.alpha, g.beta, *[_table(t, keep, n) for t in (g.a, g.b, g.bias, g.residual, g.c, g.pre8, g.a_sums)]))
+    return b"".join(packed), keep
+
+
+def canz_linear_workspace_bytes(groups: Sequence[Linear]) -> int:
+    arr, _keep = _marshal_linear(groups)
+    out = C.c_size_t(0)
+    _check(_lib.canz_linear_workspace_bytes(arr, len(groups), C.byref(out)))
+    return int(out.value)
+
+
+def canz_linear(groups: Sequence[Linear], workspace, workspace_bytes: int, stream=0) -> None:
+    """Enqueue the given products of a linear layer on ``stream``."""
+    arr, _keep = _marshal_linear(groups)
+    _check(_lib.canz_linear(arr, len(groups), _at(workspace), workspace_bytes, stream))
 
 
 def canz_profile_enable(max_launches: int) -> None:

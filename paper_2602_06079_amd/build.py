@@ -22,7 +22,8 @@ EXAMPLE_OUT = os.path.join(HERE, "c_abi_step")      # a C++ program that uses th
 
 HOST_SOURCES = ["error.cpp", "partition.cpp", "microgroup.cpp", "tp_schedule.cpp"]
 HIP_SOURCES = ["muon_step.hip", "elementwise.hip", "gemm_bf16.hip", "gemm_f32.hip", "shampoo.hip", "soap.hip",
-               "mx_step.hip", "mx_image.hip", "mx_product.hip", "mx8_image.hip", "act.hip", "norm.hip"]
+               "mx_step.hip", "mx_image.hip", "mx_product.hip", "mx8_image.hip", "act.hip", "norm.hip", "linear_step.hip", "linear_tiles.hip",
+               "linear_few.hip", "linear_edge.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 CXX = os.environ.get("CXX", "g++")

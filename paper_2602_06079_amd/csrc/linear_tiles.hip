@@ -1,0 +1,389 @@
+// Products of bf16 matrices by tiles through LDS (canz_linear): z = A B^T with either operand stored along k or across it.
+//
+// A block of four wavefronts (2 x 2) owns a tile of C, 64 W rows by 64 W columns (W = 4: 256 x 256, W = 2: 128 x 128); a wavefront has W x W tiles of
+// v_mfma_f32_32x32x16_bf16.  256 x 256 is what the accumulators allow (256 of a wavefront's 512 registers), and the larger the tile the fewer bytes go from L2 into LDS and from there into
+// registers for an operation.
+//
+// A stage holds 32 k of the tile's rows of A and of B, copied straight into LDS (a wavefront instruction moves 1 KiB; every lane names its own 16 bytes in memory, so the order in
+// LDS is free).  Four stages form a ring over the steps of all tiles of the block, one tile after another without a gap: while step t is multiplied, t + 1 .. t + 3 are there or in flight.  A
+// step has two halves of 16 k, whose operands are read into two sets of registers by turns.  The barrier lies between the halves: behind it every wavefront has read all of stage t, which
+// takes step t + 4, and has its share of stage t + 1.
+//
+// Order in LDS, so that reads have no bank conflicts:
+//   along k    rows of 32 k (64 bytes), their four 16-byte chunks turned by (row / 4) % 4: ds_read_b128 takes 8 k of a row
+//   across k   rows of k (64 W rows of the matrix side by side, 128 W bytes), their 64-byte pieces turned by k % 4: ds_read_b64_tr_b16 takes 4 k of 16 rows and hands each lane the 4 k of one
+#include <algorithm>
+#include <type_traits>
+#include <utility>
+
+#include "linear.h"
+
+namespace canz {
+namespace {
+
+constexpr int THREADS = 256;
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+#define CANZ_LDS(p) ((__attribute__((address_space(3))) void*)(p))
+#define CANZ_INLINE __attribute__((always_inline))
+#define CANZ_FENCE() __builtin_amdgcn_sched_barrier(0)
+
+template <typename F, int... I>
+__device__ __forceinline__ void static_for(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void static_for(F&& f) {
+  static_for(f, std::make_integer_sequence<int, N>{});
+}
+
+// 16 bytes a lane from base + lane_off + off straight into LDS, lane after lane; zeros for lanes whose offset is NOTHING.  The descriptor's size only tells these apart: every other
+// offset lies within the operand.  255 rows of 2^22 elements and all of k stay below it.
+constexpr unsigned ROOM = 0x7FFFF000u, NOTHING = 0x7FFFFFF0u;
+__device__ __forceinline__ void buffer_to_lds(const uint8_t* base, __attribute__((address_space(3))) void* lds, unsigned lane_off, unsigned off) {
+#if defined(__HIP_DEVICE_COMPILE__)   // the descriptor's type is the device's only
+  constexpr int RAW = 0x00027000;     // a raw buffer of dwords
+  const auto buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), static_cast<short>(0), static_cast<int>(ROOM), RAW);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer, lds, 16, static_cast<int>(lane_off), static_cast<int>(off), 0, 0);
+#endif
+}
+
+template <int W>
+struct Stage {
+  static constexpr int side = 64 * W;                  // rows of an operand
+  static constexpr int operand = side * LINEAR_K * 2;  // bytes
+  static constexpr int bytes = 2 * operand;
+  static constexpr int loads = W;                      // of one wavefront, for one operand
+};
+
+// What a block has to do and has to load next: of the launch's tiles those numbered blockIdx.x, blockIdx.x + gridDim.x, ... (tile_at)
+struct Tile {
+  int problem;   // -1: none
+  int m0, n0;
+};
+// Number `logical` of the launch's tiles.  Every XCD (blockIdx % 8, and logical % 8, since a grid has a multiple of 8 blocks) has an eighth of each product, in one piece: what its blocks
+// work on at a time is a patch of neighbours that share operands in its L2.
+constexpr int N_XCD = 8, BAND = 4;   // tile rows that are walked column by column
+template <int W>
+__device__ __forceinline__ Tile tile_at(LinearArgs ps, int logical) {
+  const int xcd = logical % N_XCD;
+  int q = logical / N_XCD;
+  for (int j = 0; j < ps->n; ++j) {
+    const int tiles = ps->first_tile[j + 1] - ps->first_tile[j];
+    const int begin = static_cast<int>(static_cast<int64_t>(tiles) * xcd / N_XCD), count = static_cast<int>(static_cast<int64_t>(tiles) * (xcd + 1) / N_XCD) - begin;
+    if (q >= count) {
+      q -= count;
+      continue;
+    }
+    const int tix = begin + q;
+    const int tiles_m = static_cast<int>((ps->pr[j].m + 64 * W - 1) / (64 * W)), tiles_n = static_cast<int>((ps->pr[j].n + 64 * W - 1) / (64 * W));
+    const int band = tix / (BAND * tiles_n), in_band = tix - band * BAND * tiles_n, rows = min(BAND, tiles_m - band * BAND);
+    const int tn = in_band / rows;
+    return Tile{j, (band * BAND + in_band - tn * rows) * 64 * W, tn * 64 * W};
+  }
+  return Tile{-1, 0, 0};
+}
+
+// One operand of the tile that is being loaded: TRANS: stored across k.
+template <int W, bool TRANS>
+struct Source {
+  using S = Stage<W>;
+  const uint8_t* base;    // of the tile's first row, k = 0
+  int64_t step_bytes;     // TRANS: from a step's first k to the next one's
+  int k;                  // of the operand
+  unsigned off[W];        // this lane's part of its pieces
+  int lane_k;             // this lane's first k of a step (TRANS: of a piece)
+
+  __device__ __forceinline__ void begin(const void* matrix, int64_t ld, int64_t extent, int first, int k_there, int wave, int lane) {
+    // TRANS: whole chunks of 8, which rows of k have (copies are padded with zeros)
+    const int there = static_cast<int>(min(TRANS ? (extent - first + 7) / 8 * 8 : extent - first, static_cast<int64_t>(S::side)));
+    k = k_there;
+    if constexpr (TRANS) {
+      base = static_cast<const uint8_t*>(matrix) + static_cast<int64_t>(first) * 2;
+      step_bytes = ld * (LINEAR_K * 2);
+      constexpr int ROW = 2 * S::side, EACH = 1024 / ROW;   // bytes of a row of k, rows of k of a piece
+      lane_k = lane * 16 / ROW;
+      const int in_row = lane * 16 % ROW;
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        const int row_k = (wave + 4 * i) * EACH + lane_k;
+        const int row = (((in_row >> 6) ^ (row_k & 3)) << 5) + (in_row & 63) / 2;
+        off[i] = static_cast<unsigned>(row_k * ld * 2 + min(row, there - 8) * 2);   // rows that are not there are read as the last
+      }
+    } else {
+      base = static_cast<const uint8_t*>(matrix) + first * ld * 2;
+      step_bytes = 0;
+      const int chunk = (lane & 3) ^ (lane >> 4 & 3);
+      lane_k = chunk * 8;
+#pragma unroll
+      for (int i = 0; i < W; ++i) off[i] = static_cast<unsigned>(min((wave + 4 * i) * 16 + lane / 4, there - 1) * ld * 2 + chunk * 16);
+    }
+  }
+  // piece i of this wavefront of step u
+  template <int I>
+  __device__ __forceinline__ void fetch(uint8_t* st, int u, int wave) const {
+    const int left = k - u * LINEAR_K;
+    if constexpr (TRANS) {
+      constexpr int EACH = 1024 / (2 * S::side);
+      buffer_to_lds(base + (left > 0 ? u : 0) * step_bytes, CANZ_LDS(st + (wave + 4 * I) * 1024), lane_k < left - (wave + 4 * I) * EACH ? off[I] : NOTHING, 0);
+    } else {
+      buffer_to_lds(base, CANZ_LDS(st + (wave + 4 * I) * 1024), lane_k < left ? off[I] : NOTHING, left > 0 ? u * (LINEAR_K * 2) : 0);
+    }
+  }
+  __device__ __forceinline__ void none() { k = 0; }
+};
+
+// A wavefront's operand of 32 rows and 16 k from a stage: lane l has 8 consecutive k (from 8 (l / 32) on) of row l % 32.
+template <int W, bool TRANS>
+struct Reader {
+  int at[TRANS ? 4 : 2];   // this lane's offsets in the operand's part of a stage
+
+  __device__ __forceinline__ void begin(int side, int lane) {   // side: which of the block's two parts of 32 W rows
+    if constexpr (TRANS) {
+      const int l = lane & 15, k = 8 * (lane >> 5) + (l >> 2);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const int piece = side * W + t;   // of 32 rows; W = 2: t 0 and 1 alone are used
+        at[t] = k * (128 * W) + ((piece ^ (l >> 2)) << 6) + (16 * (lane >> 4 & 1) + 4 * (l & 3)) * 2;
+      }
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) at[h] = (side * 32 * W + (lane & 31)) * 64 + (((2 * h + (lane >> 5)) ^ (lane >> 2 & 3)) << 4);
+    }
+  }
+  static constexpr int reads = TRANS ? 2 : 1;   // instructions for one tile's operand
+  // tile T of the wavefront's W, half HALF of the step; PART: which of the instructions
+  template <int T, int HALF, int PART>
+  __device__ __forceinline__ void read(const uint8_t* st, s16x4 (&to)[2]) const {
+    if constexpr (TRANS) {
+      typedef __attribute__((address_space(3))) s16x4 lds_vec;
+      to[PART] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_vec*)CANZ_LDS(st + at[T] + (16 * HALF + 4 * PART) * (128 * W)));
+    } else {
+      const i32x4 v = *reinterpret_cast<const i32x4*>(st + at[HALF] + T * 32 * 64);
+      typedef int i32x2 __attribute__((ext_vector_type(2)));
+      to[0] = __builtin_bit_cast(s16x4, i32x2{v[0], v[1]}), to[1] = __builtin_bit_cast(s16x4, i32x2{v[2], v[3]});
+    }
+  }
+};
+
+template <int W, bool AT, bool BT>
+__global__ __launch_bounds__(THREADS, W == 4 ? 1 : 2) void k_linear(LinearProblems) {
+  using S = Stage<W>;
+  const LinearArgs ps = (LinearArgs)__builtin_amdgcn_kernarg_segment_ptr();
+  // one array per stage: the compiler then knows that a fetch into one stage does not alias the reads of another
+  __shared__ __attribute__((aligned(1024))) uint8_t st0[S::bytes];
+  __shared__ __attribute__((aligned(1024))) uint8_t st1[S::bytes];
+  __shared__ __attribute__((aligned(1024))) uint8_t st2[S::bytes];
+  __shared__ __attribute__((aligned(1024))) uint8_t st3[S::bytes];
+  constexpr int CW = 16 * W;                                  // columns of a piece of the wavefront's part that goes through LDS at a time
+  __shared__ __attribute__((aligned(1024))) float turn[4][32 * CW];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave >> 1, wn = wave & 1;
+
+  // ---- loading: this wavefront's pieces of the next four stages.  Every tile takes whole rounds of the ring, so its loop has no exit inside and the accumulators stay where they are;
+  // steps behind the last one give zeros.
+  Tile next_tile;   // the one that is loaded: the next one, from the last round of a tile on
+  int next_logical = blockIdx.x, load_u = 0, load_end = 0;
+  Source<W, AT> sa;
+  Source<W, BT> sb;
+  auto next_round = [&]() CANZ_INLINE {
+    load_u += 4;
+    if (load_u < load_end) return;
+    const Tile t = next_tile = tile_at<W>(ps, next_logical);
+    load_u = load_end = 0;
+    if (t.problem < 0) {   // nothing left: zeros
+      sa.none(), sb.none();
+      return;
+    }
+    next_logical += gridDim.x;
+    const auto& p = ps->pr[t.problem];
+    load_u = p.first_step, load_end = load_u + p.steps;
+    const int k_end = load_end * LINEAR_K;
+    sa.begin(p.a, p.lda, p.m, t.m0, min(p.k_a, k_end), wave, lane);
+    sb.begin(p.b, p.ldb, p.n, t.n0, min(p.k_b, k_end), wave, lane);
+  };
+  constexpr int LOADS = 2 * S::loads;
+  auto fetch_one = [&](uint8_t* st, int u, auto idx) CANZ_INLINE {
+    constexpr int I = decltype(idx)::value;
+    if constexpr (I < W)
+      sa.template fetch<I>(st, u, wave);
+    else
+      sb.template fetch<I - W>(st + S::operand, u, wave);
+  };
+
+  // ---- operands in registers: one set for each half of a step
+  Reader<W, AT> ra;
+  Reader<W, BT> rb;
+  ra.begin(wm, lane);
+  rb.begin(wn, lane);
+  s16x4 fa[2][W][2], fb[2][W][2];
+  f32x16 acc[W][W];
+  constexpr int READS_A = W * Reader<W, AT>::reads, READS = READS_A + W * Reader<W, BT>::reads;
+  auto read_one = [&](const uint8_t* st, auto half, auto idx) CANZ_INLINE {
+    constexpr int H = decltype(half)::value, I = decltype(idx)::value;
+    if constexpr (I < READS_A) {
+      constexpr int EACH = Reader<W, AT>::reads;
+      ra.template read<I / EACH, H, I % EACH>(st, fa[H][I / EACH]);
+    } else {
+      constexpr int EACH = Reader<W, BT>::reads, J = I - READS_A;
+      rb.template read<J / EACH, H, J % EACH>(st + S::operand, fb[H][J / EACH]);
+    }
+  };
+  // vmcnt(n) lgkmcnt(0)
+  constexpr auto wait_code = [](int vm) { return (vm & 15) | 0x70 | (vm >> 4) << 14; };
+
+  auto multiply = [&](auto half, auto x) CANZ_INLINE {
+    constexpr int H = decltype(half)::value, idx = decltype(x)::value, i = idx / W, j = idx % W;
+    struct Pair { s16x4 v[2]; };
+    // B first: a lane then has 4 consecutive columns of a row of C in consecutive registers
+    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, Pair{{fb[H][j][0], fb[H][j][1]}}),
+                                                        __builtin_bit_cast(bf16x8, Pair{{fa[H][i][0], fa[H][i][1]}}), acc[i][j], 0, 0, 0);
+  };
+  using Half0 = std::integral_constant<int, 0>;
+  using Half1 = std::integral_constant<int, 1>;
+  // One step: its first half is in registers; `nxt` holds the next step, `cur` takes step `u` of the next round.
+  auto step = [&](uint8_t* cur, const uint8_t* nxt, int u) CANZ_INLINE {
+    constexpr int N = W * W;
+    static_for<N>([&](auto x) CANZ_INLINE {
+      constexpr int idx = decltype(x)::value;
+      multiply(Half0{}, x);
+      static_for<(idx + 1) * READS / N - idx * READS / N>([&](auto y) CANZ_INLINE {
+        CANZ_FENCE();
+        read_one(cur, Half1{}, std::integral_constant<int, idx * READS / N + decltype(y)::value>{});
+        CANZ_FENCE();
+      });
+    });
+    CANZ_FENCE();
+    __builtin_amdgcn_s_waitcnt(wait_code(2 * LOADS));
+    __builtin_amdgcn_s_barrier();
+    CANZ_FENCE();
+    static_for<N>([&](auto x) CANZ_INLINE {
+      constexpr int idx = decltype(x)::value;
+      multiply(Half1{}, x);
+      static_for<(idx + 1) * READS / N - idx * READS / N>([&](auto y) CANZ_INLINE {
+        CANZ_FENCE();
+        read_one(nxt, Half0{}, std::integral_constant<int, idx * READS / N + decltype(y)::value>{});
+        CANZ_FENCE();
+      });
+      static_for<(idx + 1) * LOADS / N - idx * LOADS / N>([&](auto y) CANZ_INLINE {
+        CANZ_FENCE();
+        fetch_one(cur, u, std::integral_constant<int, idx * LOADS / N + decltype(y)::value>{});
+        CANZ_FENCE();
+      });
+    });
+  };
+
+  // Accumulator register r of lane l in tile (i, j) is row 32 i + l % 32, column 32 j + 8 (r / 4) + 4 (l / 32) + r % 4 of the wavefront's part.  Pieces of 32 x CW of it go through LDS, 16-byte
+  // chunks turned by the row, so that a lane has eight consecutive columns and a store instruction long pieces of rows.
+  auto store_tile = [&](const Tile& t) CANZ_INLINE {
+    int l = threadIdx.x & 63;   // opaque, or every address that depends on it is kept across the tiles
+    asm volatile("" : "+v"(l));
+    const LinearEnd e = linear_end_of(ps, t.problem);
+    const int64_t m = ps->pr[t.problem].m, n = ps->pr[t.problem].n;
+    constexpr int CHUNKS = CW / 4, COLS = CW / 8, ROWS = 64 / COLS;   // of a row; lanes along a row, rows at a time
+    float* const mine = turn[wave];
+    static_for<W>([&](auto x) CANZ_INLINE {
+      constexpr int i = decltype(x)::value;
+      static_for<2>([&](auto y) CANZ_INLINE {
+        constexpr int q = decltype(y)::value, EACH = W / 2;
+        static_for<EACH>([&](auto z) CANZ_INLINE {
+          constexpr int jj = decltype(z)::value, j = q * EACH + jj;
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const int chunk = (jj * 8 + 2 * g + (l >> 5)) ^ (l & (CHUNKS - 1));
+            *reinterpret_cast<f32x4*>(mine + (l & 31) * CW + chunk * 4) = f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+          }
+        });
+#pragma clang loop unroll(disable)
+        for (int r0 = 0; r0 < 32; r0 += ROWS) {
+          const int r = r0 + l / COLS, c = l % COLS;
+          const f32x4 lo = *reinterpret_cast<const f32x4*>(mine + r * CW + ((2 * c) ^ (r & (CHUNKS - 1))) * 4);
+          const f32x4 hi = *reinterpret_cast<const f32x4*>(mine + r * CW + ((2 * c + 1) ^ (r & (CHUNKS - 1))) * 4);
+          const int64_t row = t.m0 + wm * 32 * W + i * 32 + r, col = t.n0 + wn * 32 * W + q * CW + c * 8;
+          linear_end(e, row, col, n, row < m, f32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+        }
+      });
+    });
+  };
+
+  next_round();
+  if (next_tile.problem < 0) return;   // this XCD's share is one tile less than others'
+  static_for<LOADS>([&](auto idx) CANZ_INLINE { fetch_one(st0, load_u, idx); });
+  static_for<LOADS>([&](auto idx) CANZ_INLINE { fetch_one(st1, load_u + 1, idx); });
+  static_for<LOADS>([&](auto idx) CANZ_INLINE { fetch_one(st2, load_u + 2, idx); });
+  static_for<LOADS>([&](auto idx) CANZ_INLINE { fetch_one(st3, load_u + 3, idx); });
+  __builtin_amdgcn_s_waitcnt(wait_code(3 * LOADS));
+  __builtin_amdgcn_s_barrier();
+  CANZ_FENCE();
+  static_for<READS>([&](auto idx) CANZ_INLINE { read_one(st0, Half0{}, idx); });
+
+  for (;;) {
+    const Tile t = next_tile;
+    if (t.problem < 0) break;
+#pragma unroll
+    for (int i = 0; i < W; ++i)
+#pragma unroll
+      for (int j = 0; j < W; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+    for (int rounds = (ps->pr[t.problem].steps + 3) / 4; rounds > 0; --rounds) {
+      next_round();
+      step(st0, st1, load_u);
+      step(st1, st2, load_u + 1);
+      step(st2, st3, load_u + 2);
+      step(st3, st0, load_u + 3);
+    }
+    store_tile(t);
+  }
+  __builtin_amdgcn_s_waitcnt(wait_code(0));   // the requests behind the last tile have landed before the block leaves
+}
+
+// sets first_tile of every problem for tiles of `side` x `side`; the number of tiles
+int64_t count_tiles(LinearProblems& ps, int side) {
+  int64_t tiles = 0;
+  for (int i = 0; i < ps.n; ++i) {
+    ps.first_tile[i] = static_cast<int>(tiles);
+    tiles += (ps.pr[i].m + side - 1) / side * ((ps.pr[i].n + side - 1) / side);
+  }
+  ps.first_tile[ps.n] = static_cast<int>(tiles);
+  return tiles;
+}
+
+// blocks for these tiles, `most` (a multiple of 8) at a time: as many on each XCD as the one with most tiles has
+dim3 tile_grid(const LinearProblems& ps, int most) {
+  int64_t longest = 0;   // an XCD has at most an eighth of each product, rounded up
+  for (int i = 0; i < ps.n; ++i) longest += (ps.first_tile[i + 1] - ps.first_tile[i] + N_XCD - 1) / N_XCD;
+  return dim3(static_cast<unsigned>(std::min<int64_t>(N_XCD * longest, most)));
+}
+
+template <int W>
+void launch(const LinearProblems& ps, bool at, bool bt, dim3 grid, hipStream_t st) {
+  if (at && bt)
+    k_linear<W, true, true><<<grid, THREADS, 0, st>>>(ps);
+  else if (at)
+    k_linear<W, true, false><<<grid, THREADS, 0, st>>>(ps);
+  else if (bt)
+    k_linear<W, false, true><<<grid, THREADS, 0, st>>>(ps);
+  else
+    k_linear<W, false, false><<<grid, THREADS, 0, st>>>(ps);
+}
+
+}  // namespace
+
+hipError_t launch_linear_tiles(LinearProblems& ps, bool a_trans, bool b_trans, hipStream_t st) {
+  std::sort(ps.pr, ps.pr + ps.n, [](const LinearProblem& x, const LinearProblem& y) { return x.steps > y.steps; });   // the longest begin
+  const int64_t large = count_tiles(ps, 256), small = count_tiles(ps, 128);
+  int64_t steps = 0;   // of all small tiles
+  for (int i = 0; i < ps.n; ++i) steps += static_cast<int64_t>(ps.first_tile[i + 1] - ps.first_tile[i]) * ps.pr[i].steps;
+  if (linear_large_tiles(large, small, (steps + small - 1) / small)) {
+    count_tiles(ps, 256);
+    launch<4>(ps, a_trans, b_trans, tile_grid(ps, LINEAR_CU), st);
+  } else {
+    launch<2>(ps, a_trans, b_trans, tile_grid(ps, 2 * LINEAR_CU), st);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace canz

@@ -180,3 +180,73 @@ def test_norm_refusals(canz):
     canz.canz_norm_backward([canz.NormGrad(rows=5, cols=0)], 0, 0, 0)
     assert b(rows=0, dx=None, dweight=None) == canz.EINVAL
     assert b(rows=0, ws=0) == canz.EWORKSPACE          # dweight <- beta dweight is left to do
+
+
+def test_linear_struct_layout(canz):
+    assert [(f, ctypes.sizeof(t)) for f, t in canz._Linear._fields_] == _struct_fields("canz_linear_group")
+
+
+def test_linear_refusals_and_workspace(canz):
+    P = canz.Linear
+    ok = dict(m=80, n=128, k=256, a=[4096], b=[8192], c=[12288])
+
+    def p(ws=256 * 1024, ws_bytes=1 << 40, **kw):
+        return _code(canz, canz.canz_linear, [P(**{**ok, **kw})], ws, ws_bytes, 0)
+
+    assert p(a=[4097]) == canz.EINVAL
+    assert p(b=[8193]) == canz.EINVAL
+    assert p(a=[4096 + 64], a_dtype=canz.DT_MX8) == canz.EINVAL
+    assert p(b=[8192 + 128], b_dtype=canz.DT_MX8) == canz.EINVAL
+    assert p(a=[0]) == canz.EINVAL
+    assert p(c=[0]) == canz.EINVAL
+    assert p(c=[12290], out_dtype=canz.DT_F32) == canz.EINVAL
+    assert p(bias=[0]) == canz.EINVAL
+    assert p(bias=[4098]) == canz.EINVAL
+    assert p(residual=[0]) == canz.EINVAL
+    assert p(residual=[4097]) == canz.EINVAL
+    assert p(residual=[16384], ldr=127) == canz.EINVAL
+    assert p(residual=[12288], ldr=129) == canz.EINVAL and "another row distance" in canz.canz_last_error()
+    assert p(pre8=[16384 + 16]) == canz.EINVAL
+    assert p(a_sums=[16386]) == canz.EINVAL
+    assert p(a_sums=[0]) == canz.EINVAL
+    assert p(a=[], n_prods=1) == canz.EINVAL
+    assert p(m=-1) == canz.EINVAL
+    assert p(ldc=127) == canz.EINVAL
+    assert p(lda=255) == canz.EINVAL
+    assert p(lda=79, a_trans=True) == canz.EINVAL
+    assert p(ldb=127, b_trans=True) == canz.EINVAL
+    assert p(a_trans=2) == canz.EINVAL
+    assert p(b_trans=-1) == canz.EINVAL
+    assert p(n_prods=-2, a=[], b=[], c=[]) == canz.EINVAL
+    assert p(n=4194241) == canz.ESHAPE
+    assert p(n=4194240, k=4194240) == canz.ESHAPE
+    assert p(a_dtype=canz.DT_F32) == canz.EUNSUPPORTED
+    assert p(b_dtype=canz.DT_MX) == canz.EUNSUPPORTED
+    assert p(out_dtype=canz.DT_MX8) == canz.EUNSUPPORTED
+    assert p(bias_dtype=canz.DT_MX8) == canz.EUNSUPPORTED
+    assert p(act=4) == canz.EUNSUPPORTED
+    assert p(ws=0) == canz.EWORKSPACE
+    assert p(ws=256 + 16) == canz.EWORKSPACE
+    assert p(ws_bytes=255) == canz.EWORKSPACE
+    # operands that lie well need nothing, others a copy of their own, and so do tables that are not given
+    w = canz.canz_linear_workspace_bytes
+    base = w([P(**ok)])
+    assert base >= 256
+    assert w([P(**{**ok, "a": [4098]})]) >= base + 80 * 256 * 2 - 256
+    assert w([P(**{**ok, "ldb": 257})]) >= base + 128 * 256 * 2 - 256
+    assert w([P(m=80, n=128, k=256, n_prods=1)]) >= base + (80 + 128) * 256 * 2 - 512
+    assert w([P(m=64, n=128, k=257, n_prods=1)]) == 256                       # few rows are read where they lie
+    assert w([P(m=64, n=128, k=257, n_prods=3, b_dtype=canz.DT_MX8)]) >= 3 * 128 * 257 * 2
+    assert p(a=[4098], ws_bytes=w([P(**{**ok, "a": [4098]})]) - 1) == canz.EWORKSPACE
+    assert "workspace too small" in canz.canz_last_error()
+    assert w([]) == 256
+    assert _code(canz, w, [P(m=1, n=1, k=-1, n_prods=1)]) == canz.EINVAL
+    many = dict(m=1 << 18, n=128, k=1 << 19, n_prods=(1 << 31) - 1)
+    assert _code(canz, w, [P(**many)]) == canz.ESHAPE
+    # a later group that is wrong stops the call before the first is enqueued (no device here: a launch would fail otherwise)
+    assert _code(canz, canz.canz_linear, [P(**ok), P(**{**ok, "ldc": 1})], 256 * 1024, 1 << 40, 0) == canz.EINVAL
+    with pytest.raises(ValueError):
+        canz.canz_linear([P(**{**ok, "bias": [4096, 4096]})], 256 * 1024, 1 << 40, 0)
+    # nothing to do: neither pointers nor a workspace are looked at
+    canz.canz_linear([], 0, 0, 0)
+    canz.canz_linear([P(m=0, n=5, k=5, n_prods=2), P(m=5, n=0, k=5, n_prods=2), P(m=5, n=5, k=5, n_prods=0)], 0, 0, 0)
