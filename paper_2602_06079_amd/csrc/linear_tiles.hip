@@ -1,17 +1,19 @@
 // Products of bf16 matrices by tiles through LDS (canz_linear): z = A B^T with either operand stored along k or across it.
 //
-// A block of four wavefronts (2 x 2) owns a tile of C, 64 W rows by 64 W columns (W = 4: 256 x 256, W = 2: 128 x 128); a wavefront has W x W tiles of
-// v_mfma_f32_32x32x16_bf16.  256 x 256 is what the accumulators allow (256 of a wavefront's 512 registers), and the larger the tile the fewer bytes go from L2 into LDS and from there into
-// registers for an operation.
+// A block of four wavefronts (2 x 2) owns a tile of C, 64 W rows by 64 W columns (W = 4: 256 x 256, W = 2: 128 x 128); a wavefront has 2 W x 2 W tiles of
+// v_mfma_f32_16x16x32_bf16.  256 x 256 is what the accumulators allow (256 of a wavefront's 512 registers), and the larger the tile the fewer bytes go from L2 into LDS and from there into
+// registers for an operation.  What bounds long products is power, and from registers alone, on normal random operands, these instructions reach 2060 TFLOP/s where the 32 x 32 x 16 ones
+// reach 1800.
 //
 // A stage holds 32 k of the tile's rows of A and of B, copied straight into LDS (a wavefront instruction moves 1 KiB; every lane names its own 16 bytes in memory, so the order in
-// LDS is free).  Four stages form a ring over the steps of all tiles of the block, one tile after another without a gap: while step t is multiplied, t + 1 .. t + 3 are there or in flight.  A
-// step has two halves of 16 k, whose operands are read into two sets of registers by turns.  The barrier lies between the halves: behind it every wavefront has read all of stage t, which
-// takes step t + 4, and has its share of stage t + 1.
+// LDS is free).  Four stages form a ring over the steps of all tiles of the block, one tile after another without a gap: while step t is multiplied from registers, the operands of t + 1 are
+// read from LDS (B's into a second set, each of A's behind the row of tiles that it was for), t + 2 and t + 3 are in flight and t + 4 is requested into the stage of t, which every wavefront
+// has read before the barrier at the start of the step.
 //
 // Order in LDS, so that reads have no bank conflicts:
 //   along k    rows of 32 k (64 bytes), their four 16-byte chunks turned by (row / 4) % 4: ds_read_b128 takes 8 k of a row
-//   across k   rows of k (64 W rows of the matrix side by side, 128 W bytes), their 64-byte pieces turned by k % 4: ds_read_b64_tr_b16 takes 4 k of 16 rows and hands each lane the 4 k of one
+//   across k   rows of k (64 W rows of the matrix side by side, 128 W bytes), their 64-byte pieces turned by k % 4 and the halves of these by (k / 8) % 2: ds_read_b64_tr_b16 takes 4 k of
+//              16 rows, and hands each lane the 4 k of one row
 #include <algorithm>
 #include <type_traits>
 #include <utility>
@@ -41,7 +43,7 @@ __device__ __forceinline__ void static_for(F&& f) {
 
 // 16 bytes a lane from base + lane_off + off straight into LDS, lane after lane; zeros for lanes whose offset is NOTHING.  The descriptor's size only tells these apart: every other
 // offset lies within the operand.  255 rows of 2^22 elements and all of k stay below it.
-constexpr unsigned ROOM = 0x7FFFF000u, NOTHING = 0x7FFFFFF0u;
+[[maybe_unused]] constexpr unsigned ROOM = 0x7FFFF000u, NOTHING = 0x7FFFFFF0u;
 __device__ __forceinline__ void buffer_to_lds(const uint8_t* base, __attribute__((address_space(3))) void* lds, unsigned lane_off, unsigned off) {
 #if defined(__HIP_DEVICE_COMPILE__)   // the descriptor's type is the device's only
   constexpr int RAW = 0x00027000;     // a raw buffer of dwords
@@ -109,7 +111,7 @@ struct Source {
 #pragma unroll
       for (int i = 0; i < W; ++i) {
         const int row_k = (wave + 4 * i) * EACH + lane_k;
-        const int row = (((in_row >> 6) ^ (row_k & 3)) << 5) + (in_row & 63) / 2;
+        const int row = (((in_row >> 6) ^ (row_k & 3)) << 5) + (((in_row >> 5 & 1) ^ (row_k >> 3 & 1)) << 4) + (in_row & 31) / 2;
         off[i] = static_cast<unsigned>(row_k * ld * 2 + min(row, there - 8) * 2);   // rows that are not there are read as the last
       }
     } else {
@@ -135,38 +137,49 @@ struct Source {
   __device__ __forceinline__ void none() { k = 0; }
 };
 
-// A wavefront's operand of 32 rows and 16 k from a stage: lane l has 8 consecutive k (from 8 (l / 32) on) of row l % 32.
+// A wavefront's operand of 16 rows and 32 k from a stage: lane l has 8 consecutive k (from 8 (l / 16) on) of row l % 16.
 template <int W, bool TRANS>
 struct Reader {
-  int at[TRANS ? 4 : 2];   // this lane's offsets in the operand's part of a stage
+  int at[TRANS ? W : 1];   // this lane's offsets in the operand's part of a stage: by pieces of 32 rows, or of the first row
 
   __device__ __forceinline__ void begin(int side, int lane) {   // side: which of the block's two parts of 32 W rows
+    const int l = lane & 15, k8 = lane >> 4;
     if constexpr (TRANS) {
-      const int l = lane & 15, k = 8 * (lane >> 5) + (l >> 2);
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const int piece = side * W + t;   // of 32 rows; W = 2: t 0 and 1 alone are used
-        at[t] = k * (128 * W) + ((piece ^ (l >> 2)) << 6) + (16 * (lane >> 4 & 1) + 4 * (l & 3)) * 2;
-      }
+      for (int t = 0; t < W; ++t)
+        at[t] = (8 * k8 + (l >> 2)) * (128 * W) + (((side * W + t) ^ (l >> 2)) << 6) + ((k8 & 1) << 5) + 8 * (l & 3);
     } else {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) at[h] = (side * 32 * W + (lane & 31)) * 64 + (((2 * h + (lane >> 5)) ^ (lane >> 2 & 3)) << 4);
+      at[0] = (side * 32 * W + l) * 64 + ((k8 ^ (l >> 2)) << 4);
     }
   }
-  static constexpr int reads = TRANS ? 2 : 1;   // instructions for one tile's operand
-  // tile T of the wavefront's W, half HALF of the step; PART: which of the instructions
-  template <int T, int HALF, int PART>
-  __device__ __forceinline__ void read(const uint8_t* st, s16x4 (&to)[2]) const {
+  // tile T of the wavefront's 2 W
+  template <int T>
+  __device__ __forceinline__ bf16x8 read(const uint8_t* st) const {
     if constexpr (TRANS) {
       typedef __attribute__((address_space(3))) s16x4 lds_vec;
-      to[PART] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_vec*)CANZ_LDS(st + at[T] + (16 * HALF + 4 * PART) * (128 * W)));
+      const uint8_t* const from = st + (at[T / 2] ^ (T % 2 * 32));   // an odd tile is the other half of its piece
+      const s16x4 v[2] = {__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_vec*)CANZ_LDS(from)), __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_vec*)CANZ_LDS(from + 4 * (128 * W)))};
+      return __builtin_bit_cast(bf16x8, v);
     } else {
-      const i32x4 v = *reinterpret_cast<const i32x4*>(st + at[HALF] + T * 32 * 64);
-      typedef int i32x2 __attribute__((ext_vector_type(2)));
-      to[0] = __builtin_bit_cast(s16x4, i32x2{v[0], v[1]}), to[1] = __builtin_bit_cast(s16x4, i32x2{v[2], v[3]});
+      return *reinterpret_cast<const bf16x8*>(st + at[0] + T * 16 * 64);
     }
   }
 };
+
+// acc += P Q^T.  ASM: accumulators that fill one half of the registers stay there, each where it is; through the builtin the compiler moves some of them around in every round, where an
+// operand is read across k.  What it knows about these instructions and does not see here: their operands come from LDS, behind a wait; the same accumulator is needed again 63 instructions
+// later; and every round ends with settle(), before anything else can read accumulators.
+template <bool ASM>
+__device__ __forceinline__ void multiply(f32x4& acc, const bf16x8& p, const bf16x8& q) {
+  if constexpr (ASM)
+    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(p), "v"(q));
+  else
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p, q, acc, 0, 0, 0);
+}
+template <bool ASM>
+__device__ __forceinline__ void settle() {
+  if constexpr (ASM) asm volatile("s_nop 15\n\ts_nop 15");   // 32 wait states, where a result of 8 passes needs 19 at most
+}
 
 template <int W, bool AT, bool BT>
 __global__ __launch_bounds__(THREADS, W == 4 ? 1 : 2) void k_linear(LinearProblems) {
@@ -213,60 +226,40 @@ __global__ __launch_bounds__(THREADS, W == 4 ? 1 : 2) void k_linear(LinearProble
       sb.template fetch<I - W>(st + S::operand, u, wave);
   };
 
-  // ---- operands in registers: one set for each half of a step
+  // ---- operands in registers: two sets of B's, which every row of tiles needs; one of A's, each of which is read anew behind its row of tiles
   Reader<W, AT> ra;
   Reader<W, BT> rb;
   ra.begin(wm, lane);
   rb.begin(wn, lane);
-  s16x4 fa[2][W][2], fb[2][W][2];
-  f32x16 acc[W][W];
-  constexpr int READS_A = W * Reader<W, AT>::reads, READS = READS_A + W * Reader<W, BT>::reads;
-  auto read_one = [&](const uint8_t* st, auto half, auto idx) CANZ_INLINE {
-    constexpr int H = decltype(half)::value, I = decltype(idx)::value;
-    if constexpr (I < READS_A) {
-      constexpr int EACH = Reader<W, AT>::reads;
-      ra.template read<I / EACH, H, I % EACH>(st, fa[H][I / EACH]);
-    } else {
-      constexpr int EACH = Reader<W, BT>::reads, J = I - READS_A;
-      rb.template read<J / EACH, H, J % EACH>(st + S::operand, fb[H][J / EACH]);
-    }
-  };
+  constexpr int T = 2 * W;   // tiles of a wavefront along either side
+  bf16x8 fa[T], fb[2][T];
+  f32x4 acc[T][T];
   // vmcnt(n) lgkmcnt(0)
   constexpr auto wait_code = [](int vm) { return (vm & 15) | 0x70 | (vm >> 4) << 14; };
 
-  auto multiply = [&](auto half, auto x) CANZ_INLINE {
-    constexpr int H = decltype(half)::value, idx = decltype(x)::value, i = idx / W, j = idx % W;
-    struct Pair { s16x4 v[2]; };
-    // B first: a lane then has 4 consecutive columns of a row of C in consecutive registers
-    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, Pair{{fb[H][j][0], fb[H][j][1]}}),
-                                                        __builtin_bit_cast(bf16x8, Pair{{fa[H][i][0], fa[H][i][1]}}), acc[i][j], 0, 0, 0);
-  };
-  using Half0 = std::integral_constant<int, 0>;
-  using Half1 = std::integral_constant<int, 1>;
-  // One step: its first half is in registers; `nxt` holds the next step, `cur` takes step `u` of the next round.
-  auto step = [&](uint8_t* cur, const uint8_t* nxt, int u) CANZ_INLINE {
-    constexpr int N = W * W;
-    static_for<N>([&](auto x) CANZ_INLINE {
-      constexpr int idx = decltype(x)::value;
-      multiply(Half0{}, x);
-      static_for<(idx + 1) * READS / N - idx * READS / N>([&](auto y) CANZ_INLINE {
-        CANZ_FENCE();
-        read_one(cur, Half1{}, std::integral_constant<int, idx * READS / N + decltype(y)::value>{});
-        CANZ_FENCE();
-      });
-    });
-    CANZ_FENCE();
+  using Set0 = std::integral_constant<int, 0>;
+  using Set1 = std::integral_constant<int, 1>;
+  // One step from register set `set`; `nxt` holds the next step, `cur` (read by everybody at the barrier) takes step `u` of the next round.
+  auto step = [&](auto set, uint8_t* cur, const uint8_t* nxt, int u) CANZ_INLINE {
+    constexpr int S_ = decltype(set)::value, N = T * T;
     __builtin_amdgcn_s_waitcnt(wait_code(2 * LOADS));
     __builtin_amdgcn_s_barrier();
     CANZ_FENCE();
     static_for<N>([&](auto x) CANZ_INLINE {
-      constexpr int idx = decltype(x)::value;
-      multiply(Half1{}, x);
-      static_for<(idx + 1) * READS / N - idx * READS / N>([&](auto y) CANZ_INLINE {
+      constexpr int idx = decltype(x)::value, i = idx / T, j = idx % T;
+      // B first: a lane then has 4 consecutive columns of a row of C; and the first operand changes from one instruction to the next while the second stays, which costs less power
+      multiply<W == 4>(acc[i][j], fb[S_][j], fa[i]);
+      if constexpr (j == T - 1) {
         CANZ_FENCE();
-        read_one(nxt, Half0{}, std::integral_constant<int, idx * READS / N + decltype(y)::value>{});
+        fa[i] = ra.template read<i>(nxt);
         CANZ_FENCE();
-      });
+      }
+      constexpr int PACE = T / 2;   // B's are there before the next step begins
+      if constexpr (idx < N / 2 && idx % PACE == 1) {
+        CANZ_FENCE();
+        fb[1 - S_][idx / PACE] = rb.template read<idx / PACE>(nxt + S::operand);
+        CANZ_FENCE();
+      }
       static_for<(idx + 1) * LOADS / N - idx * LOADS / N>([&](auto y) CANZ_INLINE {
         CANZ_FENCE();
         fetch_one(cur, u, std::integral_constant<int, idx * LOADS / N + decltype(y)::value>{});
@@ -275,7 +268,7 @@ __global__ __launch_bounds__(THREADS, W == 4 ? 1 : 2) void k_linear(LinearProble
     });
   };
 
-  // Accumulator register r of lane l in tile (i, j) is row 32 i + l % 32, column 32 j + 8 (r / 4) + 4 (l / 32) + r % 4 of the wavefront's part.  Pieces of 32 x CW of it go through LDS, 16-byte
+  // Accumulator register r of lane l in tile (i, j) is row 16 i + l % 16, column 16 j + 4 (l / 16) + r of the wavefront's part.  Pieces of 32 x CW of it go through LDS, 16-byte
   // chunks turned by the row, so that a lane has eight consecutive columns and a store instruction long pieces of rows.
   auto store_tile = [&](const Tile& t) CANZ_INLINE {
     int l = threadIdx.x & 63;   // opaque, or every address that depends on it is kept across the tiles
@@ -287,15 +280,14 @@ __global__ __launch_bounds__(THREADS, W == 4 ? 1 : 2) void k_linear(LinearProble
     static_for<W>([&](auto x) CANZ_INLINE {
       constexpr int i = decltype(x)::value;
       static_for<2>([&](auto y) CANZ_INLINE {
-        constexpr int q = decltype(y)::value, EACH = W / 2;
-        static_for<EACH>([&](auto z) CANZ_INLINE {
-          constexpr int jj = decltype(z)::value, j = q * EACH + jj;
+        constexpr int q = decltype(y)::value;
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const int chunk = (jj * 8 + 2 * g + (l >> 5)) ^ (l & (CHUNKS - 1));
-            *reinterpret_cast<f32x4*>(mine + (l & 31) * CW + chunk * 4) = f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+        for (int ii = 0; ii < 2; ++ii)
+#pragma unroll
+          for (int jj = 0; jj < W; ++jj) {
+            const int r = ii * 16 + (l & 15), chunk = (jj * 4 + (l >> 4)) ^ (r & (CHUNKS - 1));
+            *reinterpret_cast<f32x4*>(mine + r * CW + chunk * 4) = acc[2 * i + ii][q * W + jj];
           }
-        });
 #pragma clang loop unroll(disable)
         for (int r0 = 0; r0 < 32; r0 += ROWS) {
           const int r = r0 + l / COLS, c = l % COLS;
@@ -317,24 +309,28 @@ __global__ __launch_bounds__(THREADS, W == 4 ? 1 : 2) void k_linear(LinearProble
   __builtin_amdgcn_s_waitcnt(wait_code(3 * LOADS));
   __builtin_amdgcn_s_barrier();
   CANZ_FENCE();
-  static_for<READS>([&](auto idx) CANZ_INLINE { read_one(st0, Half0{}, idx); });
+  static_for<T>([&](auto idx) CANZ_INLINE {
+    constexpr int I = decltype(idx)::value;
+    fa[I] = ra.template read<I>(st0);
+    fb[0][I] = rb.template read<I>(st0 + S::operand);
+  });
 
   for (;;) {
     const Tile t = next_tile;
     if (t.problem < 0) break;
 #pragma unroll
-    for (int i = 0; i < W; ++i)
+    for (int i = 0; i < T; ++i)
 #pragma unroll
-      for (int j = 0; j < W; ++j)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-    for (int rounds = (ps->pr[t.problem].steps + 3) / 4; rounds > 0; --rounds) {
+      for (int j = 0; j < T; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    int rounds = (ps->pr[t.problem].steps + 3) / 4;   // at least one
+    do {
       next_round();
-      step(st0, st1, load_u);
-      step(st1, st2, load_u + 1);
-      step(st2, st3, load_u + 2);
-      step(st3, st0, load_u + 3);
-    }
+      step(Set0{}, st0, st1, load_u);
+      step(Set1{}, st1, st2, load_u + 1);
+      step(Set0{}, st2, st3, load_u + 2);
+      step(Set1{}, st3, st0, load_u + 3);
+      settle<W == 4>();
+    } while (--rounds > 0);
     store_tile(t);
   }
   __builtin_amdgcn_s_waitcnt(wait_code(0));   // the requests behind the last tile have landed before the block leaves
