@@ -5,13 +5,14 @@
 // registers for an operation.  What bounds long products is power, and from registers alone, on normal random operands, these instructions reach 2060 TFLOP/s where the 32 x 32 x 16 ones
 // reach 1800.
 //
-// A stage holds 32 k of the tile's rows of A and of B, copied straight into LDS (a wavefront instruction moves 1 KiB; every lane names its own 16 bytes in memory, so the order in
-// LDS is free).  Four stages form a ring over the steps of all tiles of the block, one tile after another without a gap: while step t is multiplied from registers, the operands of t + 1 are
-// read from LDS (B's into a second set, each of A's behind the row of tiles that it was for), t + 2 and t + 3 are in flight and t + 4 is requested into the stage of t, which every wavefront
-// has read before the barrier at the start of the step.
+// A stage holds 64 k of the tile's rows of A and of B, copied straight into LDS (a wavefront instruction moves 1 KiB; every lane names its own 16 bytes in memory, so the order in LDS is free,
+// and 64 k are a whole line of a row that lies along k).  Two stages are filled by turns, over the steps of all tiles of the block, one tile after another without a gap.  A stage is two
+// steps of 32 k: while a step is multiplied from registers, the operands of the next one are read from LDS, B's into a second set, each of A's behind the row of tiles that it was for.  So during a
+// stage's first step its second half is read, and behind the barrier that follows nobody needs it any more: in its second step it takes the stage after the next, which has 1.5 steps to arrive,
+// while the next one's operands are read.  One wavefront to a SIMD issues an instruction every four cycles and a matrix instruction takes 16, so what goes on beside them has to be few instructions.
 //
 // Order in LDS, so that reads have no bank conflicts:
-//   along k    rows of 32 k (64 bytes), their four 16-byte chunks turned by (row / 4) % 4: ds_read_b128 takes 8 k of a row
+//   along k    rows of 64 k (128 bytes), their eight 16-byte chunks turned by row % 8: ds_read_b128 takes 8 k of a row
 //   across k   rows of k (64 W rows of the matrix side by side, 128 W bytes), their 64-byte pieces turned by k % 4 and the halves of these by (k / 8) % 2: ds_read_b64_tr_b16 takes 4 k of
 //              16 rows, and hands each lane the 4 k of one row
 #include <algorithm>
@@ -41,23 +42,26 @@ __device__ __forceinline__ void static_for(F&& f) {
   static_for(f, std::make_integer_sequence<int, N>{});
 }
 
-// 16 bytes a lane from base + lane_off + off straight into LDS, lane after lane; zeros for lanes whose offset is NOTHING.  The descriptor's size only tells these apart: every other
-// offset lies within the operand.  255 rows of 2^22 elements and all of k stay below it.
-[[maybe_unused]] constexpr unsigned ROOM = 0x7FFFF000u, NOTHING = 0x7FFFFFF0u;
-__device__ __forceinline__ void buffer_to_lds(const uint8_t* base, __attribute__((address_space(3))) void* lds, unsigned lane_off, unsigned off) {
+// 16 bytes a lane from base + lane_off + off + IMM straight into LDS at lds + IMM, lane after lane; zeros for lanes whose lane_off + IMM is `room` or more.
+template <int IMM>
+__device__ __forceinline__ void buffer_to_lds(const uint8_t* base, unsigned room, uint8_t* lds, unsigned lane_off, unsigned off) {
 #if defined(__HIP_DEVICE_COMPILE__)   // the descriptor's type is the device's only
   constexpr int RAW = 0x00027000;     // a raw buffer of dwords
-  const auto buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), static_cast<short>(0), static_cast<int>(ROOM), RAW);
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer, lds, 16, static_cast<int>(lane_off), static_cast<int>(off), 0, 0);
+  const auto buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), static_cast<short>(0), static_cast<int>(room), RAW);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer, CANZ_LDS(lds), 16, static_cast<int>(lane_off), static_cast<int>(off), IMM, 0);
 #endif
 }
+// Operands begin SHIFT bytes behind the buffer's base, so that what IMM adds can be taken from every lane's offset.
+// Along k the descriptor's size only tells NOTHING from an offset: 255 rows of 2^22 elements, all of k and SHIFT stay below it.
+constexpr unsigned SHIFT = 4096, ROOM = 0x7FFFF000u, NOTHING = 0x7FFFF800u;
 
+constexpr int STAGE_K = 2 * LINEAR_K;
 template <int W>
 struct Stage {
-  static constexpr int side = 64 * W;                  // rows of an operand
-  static constexpr int operand = side * LINEAR_K * 2;  // bytes
+  static constexpr int side = 64 * W;                 // rows of an operand
+  static constexpr int operand = side * STAGE_K * 2;  // bytes
   static constexpr int bytes = 2 * operand;
-  static constexpr int loads = W;                      // of one wavefront, for one operand
+  static constexpr int loads = 2 * W;                 // of one wavefront, for one operand
 };
 
 // What a block has to do and has to load next: of the launch's tiles those numbered blockIdx.x, blockIdx.x + gridDim.x, ... (tile_at)
@@ -92,55 +96,66 @@ __device__ __forceinline__ Tile tile_at(LinearArgs ps, int logical) {
 template <int W, bool TRANS>
 struct Source {
   using S = Stage<W>;
-  const uint8_t* base;    // of the tile's first row, k = 0
-  int64_t step_bytes;     // TRANS: from a step's first k to the next one's
-  int k;                  // of the operand
-  unsigned off[W];        // this lane's part of its pieces
-  int lane_k;             // this lane's first k of a step (TRANS: of a piece)
+  const uint8_t* base;     // of the tile's first row, at the round's first k (TRANS) or the first one of all, less SHIFT
+  int64_t row_bytes;       // TRANS: of a row of k
+  unsigned at;             // of the round's first k
+  int left;                // k from the round's first one on
+  unsigned off[S::loads];  // this lane's part of its pieces, and SHIFT, less what the instruction adds
+  int lane_k;              // this lane's first k of a stage
 
-  __device__ __forceinline__ void begin(const void* matrix, int64_t ld, int64_t extent, int first, int k_there, int wave, int lane) {
-    // TRANS: whole chunks of 8, which rows of k have (copies are padded with zeros)
+  __device__ __forceinline__ void begin(const void* matrix, int64_t ld, int64_t extent, int first, int k_first, int k_there, int wave, int lane) {
+    // TRANS: whole chunks of 8, which rows of k have (copies are padded with zeros); rows that are not there are read as the last
     const int there = static_cast<int>(min(TRANS ? (extent - first + 7) / 8 * 8 : extent - first, static_cast<int64_t>(S::side)));
-    k = k_there;
+    left = k_there - k_first;
+    const uint8_t* const m = static_cast<const uint8_t*>(matrix) - SHIFT;
+    row_bytes = ld * 2;
     if constexpr (TRANS) {
-      base = static_cast<const uint8_t*>(matrix) + static_cast<int64_t>(first) * 2;
-      step_bytes = ld * (LINEAR_K * 2);
+      base = m + static_cast<int64_t>(first) * 2 + k_first * row_bytes;
+      at = 0, lane_k = 0;
       constexpr int ROW = 2 * S::side, EACH = 1024 / ROW;   // bytes of a row of k, rows of k of a piece
-      lane_k = lane * 16 / ROW;
       const int in_row = lane * 16 % ROW;
 #pragma unroll
-      for (int i = 0; i < W; ++i) {
-        const int row_k = (wave + 4 * i) * EACH + lane_k;
+      for (int i = 0; i < S::loads; ++i) {
+        const int row_k = (wave * S::loads + i) * EACH + lane * 16 / ROW;
         const int row = (((in_row >> 6) ^ (row_k & 3)) << 5) + (((in_row >> 5 & 1) ^ (row_k >> 3 & 1)) << 4) + (in_row & 31) / 2;
-        off[i] = static_cast<unsigned>(row_k * ld * 2 + min(row, there - 8) * 2);   // rows that are not there are read as the last
+        off[i] = static_cast<unsigned>(row_k * row_bytes + min(row, there - 8) * 2) + SHIFT - (i & 3) * 1024;
       }
     } else {
-      base = static_cast<const uint8_t*>(matrix) + first * ld * 2;
-      step_bytes = 0;
-      const int chunk = (lane & 3) ^ (lane >> 4 & 3);
+      base = m + first * row_bytes;
+      at = static_cast<unsigned>(k_first) * 2;
+      const int chunk = (lane & 7) ^ (lane >> 3);
       lane_k = chunk * 8;
 #pragma unroll
-      for (int i = 0; i < W; ++i) off[i] = static_cast<unsigned>(min((wave + 4 * i) * 16 + lane / 4, there - 1) * ld * 2 + chunk * 16);
+      for (int i = 0; i < S::loads; ++i)
+        off[i] = static_cast<unsigned>(min((wave * S::loads + i) * 8 + (lane >> 3), there - 1) * row_bytes + chunk * 16) + SHIFT - (i & 3) * 1024;
     }
   }
-  // piece i of this wavefront of step u
-  template <int I>
-  __device__ __forceinline__ void fetch(uint8_t* st, int u, int wave) const {
-    const int left = k - u * LINEAR_K;
+  __device__ __forceinline__ void next_round() {
+    left -= 2 * STAGE_K;
+    if constexpr (TRANS)
+      base += 2 * STAGE_K * row_bytes;
+    else
+      at += 2 * STAGE_K * 2;
+  }
+  // piece I of this wavefront of the round's stage ST.  Across k the descriptor ends with the last k; along k a lane whose k is not there asks for nothing.
+  template <int ST, int I>
+  __device__ __forceinline__ void fetch(uint8_t* st, int wave) const {
+    uint8_t* const to = st + (wave * S::loads + (I & ~3)) * 1024;
+    const int there = left - ST * STAGE_K;
     if constexpr (TRANS) {
-      constexpr int EACH = 1024 / (2 * S::side);
-      buffer_to_lds(base + (left > 0 ? u : 0) * step_bytes, CANZ_LDS(st + (wave + 4 * I) * 1024), lane_k < left - (wave + 4 * I) * EACH ? off[I] : NOTHING, 0);
+      const int rows = __builtin_amdgcn_readfirstlane(there > STAGE_K ? STAGE_K : there > 0 ? there : 0);   // (uniform, which the compiler may lose sight of)
+      buffer_to_lds<(I & 3) * 1024>(base + ST * STAGE_K * row_bytes, static_cast<unsigned>(rows) * static_cast<unsigned>(row_bytes) + SHIFT, to, off[I], 0);
     } else {
-      buffer_to_lds(base, CANZ_LDS(st + (wave + 4 * I) * 1024), lane_k < left ? off[I] : NOTHING, left > 0 ? u * (LINEAR_K * 2) : 0);
+      buffer_to_lds<(I & 3) * 1024>(base, ROOM, to, lane_k < there ? off[I] : NOTHING,
+                                    __builtin_amdgcn_readfirstlane(at + ST * STAGE_K * 2));
     }
   }
-  __device__ __forceinline__ void none() { k = 0; }
 };
 
 // A wavefront's operand of 16 rows and 32 k from a stage: lane l has 8 consecutive k (from 8 (l / 16) on) of row l % 16.
 template <int W, bool TRANS>
 struct Reader {
-  int at[TRANS ? W : 1];   // this lane's offsets in the operand's part of a stage: by pieces of 32 rows, or of the first row
+  int at[TRANS ? W : 2];   // this lane's offsets in the operand's part of a stage: by pieces of 32 rows, or by halves
 
   __device__ __forceinline__ void begin(int side, int lane) {   // side: which of the block's two parts of 32 W rows
     const int l = lane & 15, k8 = lane >> 4;
@@ -149,19 +164,20 @@ struct Reader {
       for (int t = 0; t < W; ++t)
         at[t] = (8 * k8 + (l >> 2)) * (128 * W) + (((side * W + t) ^ (l >> 2)) << 6) + ((k8 & 1) << 5) + 8 * (l & 3);
     } else {
-      at[0] = (side * 32 * W + l) * 64 + ((k8 ^ (l >> 2)) << 4);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) at[h] = (side * 32 * W + l) * 128 + (((4 * h + k8) ^ (l & 7)) << 4);
     }
   }
-  // tile T of the wavefront's 2 W
-  template <int T>
+  // tile T of the wavefront's 2 W, half HALF of the stage
+  template <int T, int HALF>
   __device__ __forceinline__ bf16x8 read(const uint8_t* st) const {
     if constexpr (TRANS) {
       typedef __attribute__((address_space(3))) s16x4 lds_vec;
-      const uint8_t* const from = st + (at[T / 2] ^ (T % 2 * 32));   // an odd tile is the other half of its piece
+      const uint8_t* const from = st + (at[T / 2] ^ (T % 2 * 32)) + HALF * 32 * (128 * W);   // an odd tile is the other half of its piece
       const s16x4 v[2] = {__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_vec*)CANZ_LDS(from)), __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_vec*)CANZ_LDS(from + 4 * (128 * W)))};
       return __builtin_bit_cast(bf16x8, v);
     } else {
-      return *reinterpret_cast<const bf16x8*>(st + at[0] + T * 16 * 64);
+      return *reinterpret_cast<const bf16x8*>(st + at[HALF] + T * 16 * 128);
     }
   }
 };
@@ -188,42 +204,39 @@ __global__ __launch_bounds__(THREADS, W == 4 ? 1 : 2) void k_linear(LinearProble
   // one array per stage: the compiler then knows that a fetch into one stage does not alias the reads of another
   __shared__ __attribute__((aligned(1024))) uint8_t st0[S::bytes];
   __shared__ __attribute__((aligned(1024))) uint8_t st1[S::bytes];
-  __shared__ __attribute__((aligned(1024))) uint8_t st2[S::bytes];
-  __shared__ __attribute__((aligned(1024))) uint8_t st3[S::bytes];
   constexpr int CW = 16 * W;                                  // columns of a piece of the wavefront's part that goes through LDS at a time
   __shared__ __attribute__((aligned(1024))) float turn[4][32 * CW];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1;
 
-  // ---- loading: this wavefront's pieces of the next four stages.  Every tile takes whole rounds of the ring, so its loop has no exit inside and the accumulators stay where they are;
-  // steps behind the last one give zeros.
+  // ---- loading: this wavefront's pieces of the next round, two stages.  Every tile takes whole rounds, so its loop has no exit inside and the accumulators stay where they are; what lies behind
+  // the last k gives zeros.
   Tile next_tile;   // the one that is loaded: the next one, from the last round of a tile on
-  int next_logical = blockIdx.x, load_u = 0, load_end = 0;
+  int next_logical = blockIdx.x, rounds_left = 0;
   Source<W, AT> sa;
   Source<W, BT> sb;
   auto next_round = [&]() CANZ_INLINE {
-    load_u += 4;
-    if (load_u < load_end) return;
-    const Tile t = next_tile = tile_at<W>(ps, next_logical);
-    load_u = load_end = 0;
-    if (t.problem < 0) {   // nothing left: zeros
-      sa.none(), sb.none();
+    if (--rounds_left > 0) {
+      sa.next_round(), sb.next_round();
       return;
     }
+    const Tile t = next_tile = tile_at<W>(ps, next_logical);
+    sa.left = sb.left = 0;
+    if (t.problem < 0) return;   // nothing left: zeros
     next_logical += gridDim.x;
     const auto& p = ps->pr[t.problem];
-    load_u = p.first_step, load_end = load_u + p.steps;
-    const int k_end = load_end * LINEAR_K;
-    sa.begin(p.a, p.lda, p.m, t.m0, min(p.k_a, k_end), wave, lane);
-    sb.begin(p.b, p.ldb, p.n, t.n0, min(p.k_b, k_end), wave, lane);
+    const int first = p.first_step * LINEAR_K, k_end = first + p.steps * LINEAR_K;
+    rounds_left = (p.steps + 3) / 4;
+    sa.begin(p.a, p.lda, p.m, t.m0, first, min(p.k_a, k_end), wave, lane);
+    sb.begin(p.b, p.ldb, p.n, t.n0, first, min(p.k_b, k_end), wave, lane);
   };
   constexpr int LOADS = 2 * S::loads;
-  auto fetch_one = [&](uint8_t* st, int u, auto idx) CANZ_INLINE {
-    constexpr int I = decltype(idx)::value;
-    if constexpr (I < W)
-      sa.template fetch<I>(st, u, wave);
+  auto fetch_one = [&](auto stage, uint8_t* st, auto idx) CANZ_INLINE {
+    constexpr int I = decltype(idx)::value, ST = decltype(stage)::value;
+    if constexpr (I < S::loads)
+      sa.template fetch<ST, I>(st, wave);
     else
-      sb.template fetch<I - W>(st + S::operand, u, wave);
+      sb.template fetch<ST, I - S::loads>(st + S::operand, wave);
   };
 
   // ---- operands in registers: two sets of B's, which every row of tiles needs; one of A's, each of which is read anew behind its row of tiles
@@ -237,37 +250,41 @@ __global__ __launch_bounds__(THREADS, W == 4 ? 1 : 2) void k_linear(LinearProble
   // vmcnt(n) lgkmcnt(0)
   constexpr auto wait_code = [](int vm) { return (vm & 15) | 0x70 | (vm >> 4) << 14; };
 
-  using Set0 = std::integral_constant<int, 0>;
-  using Set1 = std::integral_constant<int, 1>;
-  // One step from register set `set`; `nxt` holds the next step, `cur` (read by everybody at the barrier) takes step `u` of the next round.
-  auto step = [&](auto set, uint8_t* cur, const uint8_t* nxt, int u) CANZ_INLINE {
-    constexpr int S_ = decltype(set)::value, N = T * T;
-    __builtin_amdgcn_s_waitcnt(wait_code(2 * LOADS));
-    __builtin_amdgcn_s_barrier();
-    CANZ_FENCE();
+  using Zero = std::integral_constant<int, 0>;
+  using One = std::integral_constant<int, 1>;
+  // One step, from half HALF of a stage; the next one's operands lie in the other half, of stage `nxt`.  The second half's step fetches stage `stage` of the next round into `cur`.
+  auto step = [&](auto half, auto stage, uint8_t* cur, const uint8_t* nxt) CANZ_INLINE {
+    constexpr int H = decltype(half)::value, N = T * T;
+    if constexpr (H == 1) {
+      __builtin_amdgcn_s_waitcnt(wait_code(0));
+      __builtin_amdgcn_s_barrier();
+      CANZ_FENCE();
+    }
     static_for<N>([&](auto x) CANZ_INLINE {
       constexpr int idx = decltype(x)::value, i = idx / T, j = idx % T;
       // B first: a lane then has 4 consecutive columns of a row of C; and the first operand changes from one instruction to the next while the second stays, which costs less power
-      multiply<W == 4>(acc[i][j], fb[S_][j], fa[i]);
+      multiply<W == 4>(acc[i][j], fb[H][j], fa[i]);
       if constexpr (j == T - 1) {
         CANZ_FENCE();
-        fa[i] = ra.template read<i>(nxt);
+        fa[i] = ra.template read<i, 1 - H>(nxt);
         CANZ_FENCE();
       }
       constexpr int PACE = T / 2;   // B's are there before the next step begins
       if constexpr (idx < N / 2 && idx % PACE == 1) {
         CANZ_FENCE();
-        fb[1 - S_][idx / PACE] = rb.template read<idx / PACE>(nxt + S::operand);
+        fb[1 - H][idx / PACE] = rb.template read<idx / PACE, 1 - H>(nxt + S::operand);
         CANZ_FENCE();
       }
-      static_for<(idx + 1) * LOADS / N - idx * LOADS / N>([&](auto y) CANZ_INLINE {
-        CANZ_FENCE();
-        fetch_one(cur, u, std::integral_constant<int, idx * LOADS / N + decltype(y)::value>{});
-        CANZ_FENCE();
-      });
+      if constexpr (H == 1) {
+        constexpr auto upto = [](int n) { return n * LOADS * 2 / N < LOADS ? n * LOADS * 2 / N : LOADS; };   // in the first half, to have long to arrive
+        static_for<upto(idx + 1) - upto(idx)>([&](auto y) CANZ_INLINE {
+          CANZ_FENCE();
+          fetch_one(stage, cur, std::integral_constant<int, upto(idx) + decltype(y)::value>{});
+          CANZ_FENCE();
+        });
+      }
     });
   };
-
   // Accumulator register r of lane l in tile (i, j) is row 16 i + l % 16, column 16 j + 4 (l / 16) + r of the wavefront's part.  Pieces of 32 x CW of it go through LDS, 16-byte
   // chunks turned by the row, so that a lane has eight consecutive columns and a store instruction long pieces of rows.
   auto store_tile = [&](const Tile& t) CANZ_INLINE {
@@ -302,17 +319,15 @@ __global__ __launch_bounds__(THREADS, W == 4 ? 1 : 2) void k_linear(LinearProble
 
   next_round();
   if (next_tile.problem < 0) return;   // this XCD's share is one tile less than others'
-  static_for<LOADS>([&](auto idx) CANZ_INLINE { fetch_one(st0, load_u, idx); });
-  static_for<LOADS>([&](auto idx) CANZ_INLINE { fetch_one(st1, load_u + 1, idx); });
-  static_for<LOADS>([&](auto idx) CANZ_INLINE { fetch_one(st2, load_u + 2, idx); });
-  static_for<LOADS>([&](auto idx) CANZ_INLINE { fetch_one(st3, load_u + 3, idx); });
-  __builtin_amdgcn_s_waitcnt(wait_code(3 * LOADS));
+  static_for<LOADS>([&](auto idx) CANZ_INLINE { fetch_one(Zero{}, st0, idx); });
+  static_for<LOADS>([&](auto idx) CANZ_INLINE { fetch_one(One{}, st1, idx); });
+  __builtin_amdgcn_s_waitcnt(wait_code(LOADS));
   __builtin_amdgcn_s_barrier();
   CANZ_FENCE();
   static_for<T>([&](auto idx) CANZ_INLINE {
     constexpr int I = decltype(idx)::value;
-    fa[I] = ra.template read<I>(st0);
-    fb[0][I] = rb.template read<I>(st0 + S::operand);
+    fa[I] = ra.template read<I, 0>(st0);
+    fb[0][I] = rb.template read<I, 0>(st0 + S::operand);
   });
 
   for (;;) {
@@ -325,10 +340,10 @@ __global__ __launch_bounds__(THREADS, W == 4 ? 1 : 2) void k_linear(LinearProble
     int rounds = (ps->pr[t.problem].steps + 3) / 4;   // at least one
     do {
       next_round();
-      step(Set0{}, st0, st1, load_u);
-      step(Set1{}, st1, st2, load_u + 1);
-      step(Set0{}, st2, st3, load_u + 2);
-      step(Set1{}, st3, st0, load_u + 3);
+      step(Zero{}, Zero{}, st0, st0);
+      step(One{}, Zero{}, st0, st1);
+      step(Zero{}, One{}, st1, st1);
+      step(One{}, One{}, st1, st0);
       settle<W == 4>();
     } while (--rounds > 0);
     store_tile(t);
