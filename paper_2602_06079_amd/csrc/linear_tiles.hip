@@ -92,8 +92,8 @@ __device__ __forceinline__ Tile tile_at(LinearArgs ps, int logical) {
   return Tile{-1, 0, 0};
 }
 
-// One operand of the tile that is being loaded: TRANS: stored across k.
-template <int W, bool TRANS>
+// One operand of the tile that is being loaded: TRANS: stored across k.  MASK: stored along k, which is no multiple of 64.
+template <int W, bool TRANS, bool MASK>
 struct Source {
   using S = Stage<W>;
   const uint8_t* base;     // of the tile's first row, at the round's first k (TRANS) or the first one of all, less SHIFT
@@ -137,7 +137,8 @@ struct Source {
     else
       at += 2 * STAGE_K * 2;
   }
-  // piece I of this wavefront of the round's stage ST.  Across k the descriptor ends with the last k; along k a lane whose k is not there asks for nothing.
+  // Piece I of this wavefront of the round's stage ST.  Across k the descriptor ends with the last k; along k a stage is there or not, or (MASK) a lane whose k is not there asks for nothing:
+  // 8192^3 takes 847 us with these selects and 807 without.
   template <int ST, int I>
   __device__ __forceinline__ void fetch(uint8_t* st, int wave) const {
     uint8_t* const to = st + (wave * S::loads + (I & ~3)) * 1024;
@@ -146,8 +147,11 @@ struct Source {
       const int rows = __builtin_amdgcn_readfirstlane(there > STAGE_K ? STAGE_K : there > 0 ? there : 0);   // (uniform, which the compiler may lose sight of)
       buffer_to_lds<(I & 3) * 1024>(base + ST * STAGE_K * row_bytes, static_cast<unsigned>(rows) * static_cast<unsigned>(row_bytes) + SHIFT, to, off[I], 0);
     } else {
-      buffer_to_lds<(I & 3) * 1024>(base, ROOM, to, lane_k < there ? off[I] : NOTHING,
-                                    __builtin_amdgcn_readfirstlane(at + ST * STAGE_K * 2));
+      const unsigned from = __builtin_amdgcn_readfirstlane(at + ST * STAGE_K * 2);
+      if constexpr (MASK)
+        buffer_to_lds<(I & 3) * 1024>(base, ROOM, to, lane_k < there ? off[I] : NOTHING, from);
+      else
+        buffer_to_lds<(I & 3) * 1024>(base, __builtin_amdgcn_readfirstlane(there > 0 ? ROOM : 0u), to, off[I], from);
     }
   }
 };
@@ -184,7 +188,7 @@ struct Reader {
 
 // acc += P Q^T.  ASM: accumulators that fill one half of the registers stay there, each where it is; through the builtin the compiler moves some of them around in every round, where an
 // operand is read across k.  What it knows about these instructions and does not see here: their operands come from LDS, behind a wait; the same accumulator is needed again 63 instructions
-// later; and every round ends with settle(), before anything else can read accumulators.
+// later; and settle() follows every round, before anything else can read accumulators (it takes as long as the last instruction).
 template <bool ASM>
 __device__ __forceinline__ void multiply(f32x4& acc, const bf16x8& p, const bf16x8& q) {
   if constexpr (ASM)
@@ -194,10 +198,10 @@ __device__ __forceinline__ void multiply(f32x4& acc, const bf16x8& p, const bf16
 }
 template <bool ASM>
 __device__ __forceinline__ void settle() {
-  if constexpr (ASM) asm volatile("s_nop 15\n\ts_nop 15");   // 32 wait states, where a result of 8 passes needs 19 at most
+  if constexpr (ASM) asm volatile("s_nop 15");   // 16 wait states, where the results of instructions of 4 passes need 8, of 8 passes 12
 }
 
-template <int W, bool AT, bool BT>
+template <int W, bool AT, bool BT, bool MASK>
 __global__ __launch_bounds__(THREADS, W == 4 ? 1 : 2) void k_linear(LinearProblems) {
   using S = Stage<W>;
   const LinearArgs ps = (LinearArgs)__builtin_amdgcn_kernarg_segment_ptr();
@@ -209,24 +213,18 @@ __global__ __launch_bounds__(THREADS, W == 4 ? 1 : 2) void k_linear(LinearProble
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1;
 
-  // ---- loading: this wavefront's pieces of the next round, two stages.  Every tile takes whole rounds, so its loop has no exit inside and the accumulators stay where they are; what lies behind
-  // the last k gives zeros.
+  // ---- loading: this wavefront's pieces of the next round, two stages.  Every tile takes whole rounds; what lies behind the last k gives zeros.
   Tile next_tile;   // the one that is loaded: the next one, from the last round of a tile on
-  int next_logical = blockIdx.x, rounds_left = 0;
-  Source<W, AT> sa;
-  Source<W, BT> sb;
-  auto next_round = [&]() CANZ_INLINE {
-    if (--rounds_left > 0) {
-      sa.next_round(), sb.next_round();
-      return;
-    }
+  int next_logical = blockIdx.x;
+  Source<W, AT, MASK> sa;
+  Source<W, BT, MASK> sb;
+  auto load_next_tile = [&]() CANZ_INLINE {
     const Tile t = next_tile = tile_at<W>(ps, next_logical);
     sa.left = sb.left = 0;
     if (t.problem < 0) return;   // nothing left: zeros
     next_logical += gridDim.x;
     const auto& p = ps->pr[t.problem];
     const int first = p.first_step * LINEAR_K, k_end = first + p.steps * LINEAR_K;
-    rounds_left = (p.steps + 3) / 4;
     sa.begin(p.a, p.lda, p.m, t.m0, first, min(p.k_a, k_end), wave, lane);
     sb.begin(p.b, p.ldb, p.n, t.n0, first, min(p.k_b, k_end), wave, lane);
   };
@@ -276,15 +274,22 @@ __global__ __launch_bounds__(THREADS, W == 4 ? 1 : 2) void k_linear(LinearProble
         CANZ_FENCE();
       }
       if constexpr (H == 1) {
-        constexpr auto upto = [](int n) { return n * LOADS * 2 / N < LOADS ? n * LOADS * 2 / N : LOADS; };   // in the first half, to have long to arrive
-        static_for<upto(idx + 1) - upto(idx)>([&](auto y) CANZ_INLINE {
+        // evenly over the step: asked for in its first half, which would give them longer to arrive, they wait for one another (12288 x 4096 x 8192 735 us instead of 684)
+        static_for<(idx + 1) * LOADS / N - idx * LOADS / N>([&](auto y) CANZ_INLINE {
           CANZ_FENCE();
-          fetch_one(stage, cur, std::integral_constant<int, upto(idx) + decltype(y)::value>{});
+          fetch_one(stage, cur, std::integral_constant<int, idx * LOADS / N + decltype(y)::value>{});
           CANZ_FENCE();
         });
       }
     });
   };
+  auto round = [&]() CANZ_INLINE {
+    step(Zero{}, Zero{}, st0, st0);
+    step(One{}, Zero{}, st0, st1);
+    step(Zero{}, One{}, st1, st1);
+    step(One{}, One{}, st1, st0);
+  };
+
   // Accumulator register r of lane l in tile (i, j) is row 16 i + l % 16, column 16 j + 4 (l / 16) + r of the wavefront's part.  Pieces of 32 x CW of it go through LDS, 16-byte
   // chunks turned by the row, so that a lane has eight consecutive columns and a store instruction long pieces of rows.
   auto store_tile = [&](const Tile& t) CANZ_INLINE {
@@ -317,7 +322,7 @@ __global__ __launch_bounds__(THREADS, W == 4 ? 1 : 2) void k_linear(LinearProble
     });
   };
 
-  next_round();
+  load_next_tile();
   if (next_tile.problem < 0) return;   // this XCD's share is one tile less than others'
   static_for<LOADS>([&](auto idx) CANZ_INLINE { fetch_one(Zero{}, st0, idx); });
   static_for<LOADS>([&](auto idx) CANZ_INLINE { fetch_one(One{}, st1, idx); });
@@ -336,16 +341,19 @@ __global__ __launch_bounds__(THREADS, W == 4 ? 1 : 2) void k_linear(LinearProble
 #pragma unroll
     for (int i = 0; i < T; ++i)
 #pragma unroll
-      for (int j = 0; j < T; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    int rounds = (ps->pr[t.problem].steps + 3) / 4;   // at least one
-    do {
-      next_round();
-      step(Zero{}, Zero{}, st0, st0);
-      step(One{}, Zero{}, st0, st1);
-      step(Zero{}, One{}, st1, st1);
-      step(One{}, One{}, st1, st0);
+      for (int j = 0; j < T; ++j) {
+        acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if constexpr (W == 4) asm volatile("" : "+a"(acc[i][j]));   // zeros that the compiler does not know: it would make them anew where a tile has but one round
+      }
+    // the last round, which loads the next tile's first one, apart: with both in one loop, what the loads need is copied to and fro in every round
+    for (int rounds = (ps->pr[t.problem].steps + 3) / 4; rounds > 1; --rounds) {
+      sa.next_round(), sb.next_round();
+      round();
       settle<W == 4>();
-    } while (--rounds > 0);
+    }
+    load_next_tile();
+    round();
+    settle<W == 4>();
     store_tile(t);
   }
   __builtin_amdgcn_s_waitcnt(wait_code(0));   // the requests behind the last tile have landed before the block leaves
@@ -369,16 +377,25 @@ dim3 tile_grid(const LinearProblems& ps, int most) {
   return dim3(static_cast<unsigned>(std::min<int64_t>(N_XCD * longest, most)));
 }
 
-template <int W>
+template <int W, bool MASK>
 void launch(const LinearProblems& ps, bool at, bool bt, dim3 grid, hipStream_t st) {
   if (at && bt)
-    k_linear<W, true, true><<<grid, THREADS, 0, st>>>(ps);
+    k_linear<W, true, true, false><<<grid, THREADS, 0, st>>>(ps);
   else if (at)
-    k_linear<W, true, false><<<grid, THREADS, 0, st>>>(ps);
+    k_linear<W, true, false, MASK><<<grid, THREADS, 0, st>>>(ps);
   else if (bt)
-    k_linear<W, false, true><<<grid, THREADS, 0, st>>>(ps);
+    k_linear<W, false, true, MASK><<<grid, THREADS, 0, st>>>(ps);
   else
-    k_linear<W, false, false><<<grid, THREADS, 0, st>>>(ps);
+    k_linear<W, false, false, MASK><<<grid, THREADS, 0, st>>>(ps);
+}
+template <int W>
+void launch(const LinearProblems& ps, bool at, bool bt, dim3 grid, hipStream_t st) {
+  bool mask = false;
+  for (int i = 0; i < ps.n; ++i) mask = mask || (!at && ps.pr[i].k_a % STAGE_K != 0) || (!bt && ps.pr[i].k_b % STAGE_K != 0);
+  if (mask)
+    launch<W, true>(ps, at, bt, grid, st);
+  else
+    launch<W, false>(ps, at, bt, grid, st);
 }
 
 }  // namespace
