@@ -33,6 +33,8 @@ constexpr int LINEAR_PROBLEMS = 16;
 struct LinearProblems {
   int n;
   int first_tile[LINEAR_PROBLEMS + 1];   // of every problem, then their number
+  int from, to;                          // tiles: which of an XCD's tiles the launch has
+  int quarters;                          // tiles of 128 x 128: the launch's tiles are those of 256 x 256, in quarters
   LinearProblem pr[LINEAR_PROBLEMS];
 };
 

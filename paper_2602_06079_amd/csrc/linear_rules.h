@@ -22,6 +22,12 @@ constexpr int64_t linear_small_ns(int64_t tiles, int64_t steps) {
 }
 constexpr bool linear_large_tiles(int64_t large, int64_t small, int64_t steps) { return linear_large_ns(large, steps) < linear_small_ns(small, steps); }
 
+// Whole rounds of large tiles after which the others, less than a round, are done as quarters by small ones; 0: all are done by large ones.  An element's sum is the same in either.
+constexpr int64_t linear_whole_rounds(int64_t large, int64_t steps) {
+  const int64_t rounds = large / LINEAR_CU, rest = large % LINEAR_CU;
+  return rounds > 0 && rest > 0 && linear_small_ns(4 * rest, steps) < linear_large_ns(rest, steps) ? rounds : 0;
+}
+
 // How many parts k is cut into, each with fp32 sums of its own in the workspace, which are added up in order: products whose tiles leave most of the chip idle for long.  A
 // product alone decides, so that its sums do not depend on what shares the call.
 constexpr int LINEAR_MAX_PARTS = 8;

@@ -66,16 +66,20 @@ struct Stage {
 
 // What a block has to do and has to load next: of the launch's tiles those numbered blockIdx.x, blockIdx.x + gridDim.x, ... (tile_at)
 struct Tile {
-  int problem;   // -1: none
+  int problem;   // NONE: there is none; OUTSIDE: a quarter of a tile that lies outside of C
   int m0, n0;
 };
+constexpr int NONE = -1, OUTSIDE = -2;
 // Number `logical` of the launch's tiles.  Every XCD (blockIdx % 8, and logical % 8, since a grid has a multiple of 8 blocks) has an eighth of each product, in one piece: what its blocks
 // work on at a time is a patch of neighbours that share operands in its L2.
 constexpr int N_XCD = 8, BAND = 4;   // tile rows that are walked column by column
 template <int W>
 __device__ __forceinline__ Tile tile_at(LinearArgs ps, int logical) {
   const int xcd = logical % N_XCD;
-  int q = logical / N_XCD;
+  int q = logical / N_XCD, quarter = 0, side = 64 * W;
+  if (W == 2 && ps->quarters) quarter = q & 3, q >>= 2, side = 256;
+  q += ps->from;
+  if (q >= ps->to) return Tile{NONE, 0, 0};
   for (int j = 0; j < ps->n; ++j) {
     const int tiles = ps->first_tile[j + 1] - ps->first_tile[j];
     const int begin = static_cast<int>(static_cast<int64_t>(tiles) * xcd / N_XCD), count = static_cast<int>(static_cast<int64_t>(tiles) * (xcd + 1) / N_XCD) - begin;
@@ -84,12 +88,13 @@ __device__ __forceinline__ Tile tile_at(LinearArgs ps, int logical) {
       continue;
     }
     const int tix = begin + q;
-    const int tiles_m = static_cast<int>((ps->pr[j].m + 64 * W - 1) / (64 * W)), tiles_n = static_cast<int>((ps->pr[j].n + 64 * W - 1) / (64 * W));
+    const int tiles_m = static_cast<int>((ps->pr[j].m + side - 1) / side), tiles_n = static_cast<int>((ps->pr[j].n + side - 1) / side);
     const int band = tix / (BAND * tiles_n), in_band = tix - band * BAND * tiles_n, rows = min(BAND, tiles_m - band * BAND);
     const int tn = in_band / rows;
-    return Tile{j, (band * BAND + in_band - tn * rows) * 64 * W, tn * 64 * W};
+    const int m0 = (band * BAND + in_band - tn * rows) * side + (quarter >> 1) * 128, n0 = tn * side + (quarter & 1) * 128;
+    return Tile{m0 < ps->pr[j].m && n0 < ps->pr[j].n ? j : OUTSIDE, m0, n0};
   }
-  return Tile{-1, 0, 0};
+  return Tile{NONE, 0, 0};
 }
 
 // One operand of the tile that is being loaded: TRANS: stored across k.  MASK: stored along k, which is no multiple of 64.
@@ -219,10 +224,14 @@ __global__ __launch_bounds__(THREADS, W == 4 ? 1 : 2) void k_linear(LinearProble
   Source<W, AT, MASK> sa;
   Source<W, BT, MASK> sb;
   auto load_next_tile = [&]() CANZ_INLINE {
-    const Tile t = next_tile = tile_at<W>(ps, next_logical);
+    Tile t;
+    do {
+      t = tile_at<W>(ps, next_logical);
+      next_logical += gridDim.x;
+    } while (W == 2 && t.problem == OUTSIDE);
+    next_tile = t;
     sa.left = sb.left = 0;
     if (t.problem < 0) return;   // nothing left: zeros
-    next_logical += gridDim.x;
     const auto& p = ps->pr[t.problem];
     const int first = p.first_step * LINEAR_K, k_end = first + p.steps * LINEAR_K;
     sa.begin(p.a, p.lda, p.m, t.m0, first, min(p.k_a, k_end), wave, lane);
@@ -370,12 +379,14 @@ int64_t count_tiles(LinearProblems& ps, int side) {
   return tiles;
 }
 
-// blocks for these tiles, `most` (a multiple of 8) at a time: as many on each XCD as the one with most tiles has
-dim3 tile_grid(const LinearProblems& ps, int most) {
-  int64_t longest = 0;   // an XCD has at most an eighth of each product, rounded up
+// An XCD has at most this many of the tiles: an eighth of each product, rounded up.
+int longest_share(const LinearProblems& ps) {
+  int64_t longest = 0;
   for (int i = 0; i < ps.n; ++i) longest += (ps.first_tile[i + 1] - ps.first_tile[i] + N_XCD - 1) / N_XCD;
-  return dim3(static_cast<unsigned>(std::min<int64_t>(N_XCD * longest, most)));
+  return static_cast<int>(longest);
 }
+// Blocks for `each` tiles on every XCD, `most` (a multiple of 8) at a time.
+dim3 tile_grid(int64_t each, int most) { return dim3(static_cast<unsigned>(std::min<int64_t>(N_XCD * each, most))); }
 
 template <int W, bool MASK>
 void launch(const LinearProblems& ps, bool at, bool bt, dim3 grid, hipStream_t st) {
@@ -405,11 +416,19 @@ hipError_t launch_linear_tiles(LinearProblems& ps, bool a_trans, bool b_trans, h
   const int64_t large = count_tiles(ps, 256), small = count_tiles(ps, 128);
   int64_t steps = 0;   // of all small tiles
   for (int i = 0; i < ps.n; ++i) steps += static_cast<int64_t>(ps.first_tile[i + 1] - ps.first_tile[i]) * ps.pr[i].steps;
-  if (linear_large_tiles(large, small, (steps + small - 1) / small)) {
-    count_tiles(ps, 256);
-    launch<4>(ps, a_trans, b_trans, tile_grid(ps, LINEAR_CU), st);
-  } else {
-    launch<2>(ps, a_trans, b_trans, tile_grid(ps, 2 * LINEAR_CU), st);
+  steps = (steps + small - 1) / small;
+  ps.from = 0, ps.to = longest_share(ps), ps.quarters = 0;
+  if (!linear_large_tiles(large, small, steps)) {
+    launch<2>(ps, a_trans, b_trans, tile_grid(ps.to, 2 * LINEAR_CU), st);
+    return hipGetLastError();
+  }
+  count_tiles(ps, 256);
+  const int all = longest_share(ps), whole = static_cast<int>(linear_whole_rounds(large, steps)) * (LINEAR_CU / N_XCD);
+  ps.to = whole > 0 ? std::min(whole, all) : all;
+  launch<4>(ps, a_trans, b_trans, tile_grid(ps.to, LINEAR_CU), st);
+  if (ps.to < all) {   // what the last round would leave most CUs without
+    ps.from = ps.to, ps.to = all, ps.quarters = 1;
+    launch<2>(ps, a_trans, b_trans, tile_grid(4 * (ps.to - ps.from), 2 * LINEAR_CU), st);
   }
   return hipGetLastError();
 }
