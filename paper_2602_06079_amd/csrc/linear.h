@@ -1,5 +1,7 @@
 // Launchers behind canz_linear (internal, not part of the ABI).
 #pragma once
+#include <type_traits>
+
 #include "act.h"
 #include "linear_rules.h"
 #include "mx8.h"
@@ -81,45 +83,65 @@ __device__ __forceinline__ LinearEnd linear_end_of(LinearArgs ps, int j) {
   return LinearEnd{e.c, e.r, e.bias, Image8{e.pre.codes, e.pre.scales, e.pre.pitch}, e.ldc, e.ldr, e.alpha, e.beta, e.act, e.out_f32, e.bias_f32};
 }
 
-// z = alpha sum + bias;  C = act(z) + beta R.  `col` is a multiple of 8, the lane's quad holds the 32 columns of a block and is active as a whole; what is not `there` (or behind n) is
-// not read or written.
-__device__ __forceinline__ void linear_end(const LinearEnd& e, int64_t row, int64_t col, int64_t n, bool there, f32x8 sum) {
-  const int64_t left = there ? n - col : 0;
-  f32x8 z;
+// z = alpha sum + bias;  C = act(z) + beta R, for eight columns (from `col` on, a multiple of 8) of the rows row, row + step, ... , R of them, m and n rows and columns of C.  The lane's quad
+// holds the 32 columns of a block and is active as a whole; what is not there is not read or written (WHOLE: all of it is).  Rows go through every part together, so that their loads are in
+// flight at once and a part's branch is taken once.
+template <bool WHOLE, int R>
+__device__ __forceinline__ void linear_end(const LinearEnd& e, int64_t row, int step, int64_t col, int64_t m, int64_t n, f32x8 (&z)[R]) {
+  const int64_t there = WHOLE ? PIECE : n - col;
+  auto left = [&](int r) { return WHOLE || row + r * step < m ? there : int64_t{0}; };
   if (e.bias) {
-    const f32x8 b = e.bias_f32 ? widen(load_raw(static_cast<const float*>(e.bias) + col, left)) : widen(load_raw(static_cast<const __bf16*>(e.bias) + col, left));
+    const f32x8 b = e.bias_f32 ? widen(load_raw(static_cast<const float*>(e.bias) + col, there)) : widen(load_raw(static_cast<const __bf16*>(e.bias) + col, there));
 #pragma unroll
-    for (int i = 0; i < PIECE; ++i) z[i] = __builtin_fmaf(e.alpha, sum[i], b[i]);
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int i = 0; i < PIECE; ++i) z[r][i] = __builtin_fmaf(e.alpha, z[r][i], b[i]);
   } else {
 #pragma unroll
-    for (int i = 0; i < PIECE; ++i) z[i] = e.alpha * sum[i];
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int i = 0; i < PIECE; ++i) z[r][i] *= e.alpha;
   }
   if (e.pre.codes) {
-    f32x8 kept = z;
 #pragma unroll
-    for (int i = 0; i < PIECE; ++i) kept[i] = i < left ? z[i] : 0.f;
-    const Codes8 c = round8(kept);
-    const Image8 im{e.pre.codes, e.pre.scales, e.pre.pitch};
-    if (there && col < im.pitch) store_codes(im, row, col, n, c);
-  }
-  if (left <= 0) return;
-  if (e.act == CANZ_ACT_SILU) {
+    for (int r = 0; r < R; ++r) {
+      f32x8 kept = z[r];
+      if constexpr (!WHOLE) {
 #pragma unroll
-    for (int i = 0; i < PIECE; ++i) z[i] = act_both<CANZ_ACT_SILU>(z[i]).value;
-  } else if (e.act == CANZ_ACT_GELU) {
-#pragma unroll
-    for (int i = 0; i < PIECE; ++i) z[i] = act_both<CANZ_ACT_GELU>(z[i]).value;
-  } else if (e.act == CANZ_ACT_RELU) {
-#pragma unroll
-    for (int i = 0; i < PIECE; ++i) z[i] = act_both<CANZ_ACT_RELU>(z[i]).value;
-  }
-  auto out = [&](auto* c, const auto* r) {
-    if (e.beta != 0.f) {
-      const f32x8 old = widen(load_raw(r + row * e.ldr + col, left));
-#pragma unroll
-      for (int i = 0; i < PIECE; ++i) z[i] = __builtin_fmaf(e.beta, old[i], z[i]);
+        for (int i = 0; i < PIECE; ++i) kept[i] = i < there ? kept[i] : 0.f;
+      }
+      const Codes8 c = round8(kept);
+      if (WHOLE || (row + r * step < m && col < e.pre.pitch)) store_codes(e.pre, row + r * step, col, n, c);
     }
-    store_piece8(c + row * e.ldc + col, left, z);
+  }
+  auto apply = [&](auto kind) {
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int i = 0; i < PIECE; ++i) z[r][i] = act_both<decltype(kind)::value>(z[r][i]).value;
+  };
+  if (e.act == CANZ_ACT_SILU)
+    apply(std::integral_constant<int, CANZ_ACT_SILU>{});
+  else if (e.act == CANZ_ACT_GELU)
+    apply(std::integral_constant<int, CANZ_ACT_GELU>{});
+  else if (e.act == CANZ_ACT_RELU)
+    apply(std::integral_constant<int, CANZ_ACT_RELU>{});
+  auto out = [&](auto* c, const auto* old) {
+    using E = std::remove_pointer_t<decltype(c)>;
+    if (e.beta != 0.f) {
+      Raw<E> x[R];
+#pragma unroll
+      for (int r = 0; r < R; ++r) x[r] = load_raw(old + (row + r * step) * e.ldr + col, left(r));
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const f32x8 v = widen(x[r]);
+#pragma unroll
+        for (int i = 0; i < PIECE; ++i) z[r][i] = __builtin_fmaf(e.beta, v[i], z[r][i]);
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (WHOLE || left(r) > 0) store_piece8(c + (row + r * step) * e.ldc + col, left(r), z[r]);
   };
   if (e.out_f32)
     out(static_cast<float*>(e.c), static_cast<const float*>(e.r));

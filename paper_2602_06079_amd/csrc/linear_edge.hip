@@ -49,7 +49,8 @@ __global__ __launch_bounds__(EACH_THREADS) void k_linear_join(LinearEnd e, int64
     for (int q = 0; q < LINEAR_MAX_PARTS; ++q)
       if (q < parts) v += part[q].v;
   }
-  linear_end(e, s.row, s.col, n, there, v);
+  f32x8 z[1] = {v};
+  linear_end<false, 1>(e, s.row, 0, s.col, m, n, z);
 }
 
 // ---- sums of A's rows -----------------------------------------------------------------------------------------------------------

@@ -152,7 +152,8 @@ __global__ __launch_bounds__(64 * WAVES) void k_linear_few(LinearProblems) {
     f32x4 lo = sums[0][tile][from], hi = sums[0][tile][from + 16];
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) lo += sums[w][tile][from], hi += sums[w][tile][from + 16];
-    linear_end(e, row, col0 + c * 8, n, row < m, f32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+    f32x8 z[1] = {f32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}};
+    linear_end<false, 1>(e, row, 0, col0 + c * 8, m, n, z);
   }
 }
 

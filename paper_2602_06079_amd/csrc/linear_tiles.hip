@@ -308,10 +308,12 @@ __global__ __launch_bounds__(THREADS, W == 4 ? 1 : 2) void k_linear(LinearProble
     const int64_t m = ps->pr[t.problem].m, n = ps->pr[t.problem].n;
     constexpr int CHUNKS = CW / 4, COLS = CW / 8, ROWS = 64 / COLS;   // of a row; lanes along a row, rows at a time
     float* const mine = turn[wave];
-    static_for<W>([&](auto x) CANZ_INLINE {
-      constexpr int i = decltype(x)::value;
-      static_for<2>([&](auto y) CANZ_INLINE {
-        constexpr int q = decltype(y)::value;
+    // One copy of what is done to a piece: a copy for each, 100 KB of instructions that a tile goes through once, took 15 us a tile, most of it waiting for them.
+#pragma clang loop unroll(disable)
+    for (int piece = 0; piece < 2 * W; ++piece) {
+      static_for<2 * W>([&](auto x) CANZ_INLINE {
+        constexpr int P = decltype(x)::value, i = P / 2, q = P % 2;
+        if (piece != P) return;
 #pragma unroll
         for (int ii = 0; ii < 2; ++ii)
 #pragma unroll
@@ -319,16 +321,26 @@ __global__ __launch_bounds__(THREADS, W == 4 ? 1 : 2) void k_linear(LinearProble
             const int r = ii * 16 + (l & 15), chunk = (jj * 4 + (l >> 4)) ^ (r & (CHUNKS - 1));
             *reinterpret_cast<f32x4*>(mine + r * CW + chunk * 4) = acc[2 * i + ii][q * W + jj];
           }
-#pragma clang loop unroll(disable)
-        for (int r0 = 0; r0 < 32; r0 += ROWS) {
-          const int r = r0 + l / COLS, c = l % COLS;
+        asm volatile("; piece %0" ::"n"(P));   // apart, or the stores are merged into one of an accumulator by its number, and the accumulators go to memory
+      });
+      const int64_t row0 = t.m0 + wm * 32 * W + (piece >> 1) * 32 + l / COLS, col0 = t.n0 + wn * 32 * W + (piece & 1) * CW, col = col0 + l % COLS * 8;
+      constexpr int R = 32 / ROWS;
+      auto finish = [&](auto whole) CANZ_INLINE {
+        f32x8 z[R];
+#pragma unroll
+        for (int x = 0; x < R; ++x) {
+          const int r = x * ROWS + l / COLS, c = l % COLS;
           const f32x4 lo = *reinterpret_cast<const f32x4*>(mine + r * CW + ((2 * c) ^ (r & (CHUNKS - 1))) * 4);
           const f32x4 hi = *reinterpret_cast<const f32x4*>(mine + r * CW + ((2 * c + 1) ^ (r & (CHUNKS - 1))) * 4);
-          const int64_t row = t.m0 + wm * 32 * W + i * 32 + r, col = t.n0 + wn * 32 * W + q * CW + c * 8;
-          linear_end(e, row, col, n, row < m, f32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+          z[x] = f32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
         }
-      });
-    });
+        linear_end<decltype(whole)::value, R>(e, row0, ROWS, col, m, n, z);
+      };
+      if (t.m0 + 64 * W <= m && t.n0 + 64 * W <= n)
+        finish(std::true_type{});
+      else
+        finish(std::false_type{});
+    }
   };
 
   load_next_tile();
