@@ -6,7 +6,7 @@
 // reach 1800.
 //
 // A stage holds 64 k of the tile's rows of A and of B, copied straight into LDS (a wavefront instruction moves 1 KiB; every lane names its own 16 bytes in memory, so the order in LDS is free,
-// and 64 k are a whole line of a row that lies along k).  Two stages are filled by turns, over the steps of all tiles of the block, one tile after another without a gap.  A stage is two
+// and 64 k are a whole line of a row that lies along k).  Two stages (or four) are filled by turns, over the steps of all tiles of the block, one tile after another without a gap.  A stage is two
 // steps of 32 k: while a step is multiplied from registers, the operands of the next one are read from LDS, B's into a second set, each of A's behind the row of tiles that it was for.  So during a
 // stage's first step its second half is read, and behind the barrier that follows nobody needs it any more: in its second step it takes the stage after the next, which has 1.5 steps to arrive,
 // while the next one's operands are read.  One wavefront to a SIMD issues an instruction every four cycles and a matrix instruction takes 16, so what goes on beside them has to be few instructions.
@@ -135,12 +135,13 @@ struct Source {
         off[i] = static_cast<unsigned>(min((wave * S::loads + i) * 8 + (lane >> 3), there - 1) * row_bytes + chunk * 16) + SHIFT - (i & 3) * 1024;
     }
   }
+  template <int STAGES>
   __device__ __forceinline__ void next_round() {
-    left -= 2 * STAGE_K;
+    left -= STAGES * STAGE_K;
     if constexpr (TRANS)
-      base += 2 * STAGE_K * row_bytes;
+      base += STAGES * STAGE_K * row_bytes;
     else
-      at += 2 * STAGE_K * 2;
+      at += STAGES * STAGE_K * 2;
   }
   // Piece I of this wavefront of the round's stage ST.  Across k the descriptor ends with the last k; along k a stage is there or not, or (MASK) a lane whose k is not there asks for nothing:
   // 8192^3 takes 847 us with these selects and 807 without.
@@ -206,19 +207,26 @@ __device__ __forceinline__ void settle() {
   if constexpr (ASM) asm volatile("s_nop 15");   // 16 wait states, where the results of instructions of 4 passes need 8, of 8 passes 12
 }
 
-template <int W, bool AT, bool BT, bool MASK>
-__global__ __launch_bounds__(THREADS, W == 4 ? 1 : 2) void k_linear(LinearProblems) {
+// STAGES: of the ring.  Where small tiles leave a CU with one block, whose steps are short, four of them give what is on its way as long as it needs.
+template <int W, int STAGES, bool AT, bool BT, bool MASK>
+__global__ __launch_bounds__(THREADS, W == 2 && STAGES == 2 ? 2 : 1) void k_linear(LinearProblems) {
   using S = Stage<W>;
   const LinearArgs ps = (LinearArgs)__builtin_amdgcn_kernarg_segment_ptr();
   // one array per stage: the compiler then knows that a fetch into one stage does not alias the reads of another
   __shared__ __attribute__((aligned(1024))) uint8_t st0[S::bytes];
   __shared__ __attribute__((aligned(1024))) uint8_t st1[S::bytes];
+  __shared__ __attribute__((aligned(1024))) uint8_t st2[STAGES > 2 ? S::bytes : 16];
+  __shared__ __attribute__((aligned(1024))) uint8_t st3[STAGES > 2 ? S::bytes : 16];
+  auto stage_at = [&](auto number) CANZ_INLINE -> uint8_t* {
+    constexpr int N = decltype(number)::value % STAGES;
+    return N == 0 ? st0 : N == 1 ? st1 : N == 2 ? st2 : st3;
+  };
   constexpr int CW = 16 * W;                                  // columns of a piece of the wavefront's part that goes through LDS at a time
   __shared__ __attribute__((aligned(1024))) float turn[4][32 * CW];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1;
 
-  // ---- loading: this wavefront's pieces of the next round, two stages.  Every tile takes whole rounds; what lies behind the last k gives zeros.
+  // ---- loading: this wavefront's pieces of the next round, all of its stages.  Every tile takes whole rounds; what lies behind the last k gives zeros.
   Tile next_tile;   // the one that is loaded: the next one, from the last round of a tile on
   int next_logical = blockIdx.x;
   Source<W, AT, MASK> sa;
@@ -259,11 +267,13 @@ __global__ __launch_bounds__(THREADS, W == 4 ? 1 : 2) void k_linear(LinearProble
 
   using Zero = std::integral_constant<int, 0>;
   using One = std::integral_constant<int, 1>;
-  // One step, from half HALF of a stage; the next one's operands lie in the other half, of stage `nxt`.  The second half's step fetches stage `stage` of the next round into `cur`.
-  auto step = [&](auto half, auto stage, uint8_t* cur, const uint8_t* nxt) CANZ_INLINE {
+  // One step, from half HALF of stage `stage`; the next one's operands lie in its other half, or in the next stage.  The second half's step fetches the stage of the next round.
+  auto step = [&](auto half, auto stage) CANZ_INLINE {
     constexpr int H = decltype(half)::value, N = T * T;
+    uint8_t* const cur = stage_at(stage);
+    const uint8_t* const nxt = stage_at(std::integral_constant<int, decltype(stage)::value + H>{});
     if constexpr (H == 1) {
-      __builtin_amdgcn_s_waitcnt(wait_code(0));
+      __builtin_amdgcn_s_waitcnt(wait_code((STAGES - 2) * LOADS));
       __builtin_amdgcn_s_barrier();
       CANZ_FENCE();
     }
@@ -293,10 +303,10 @@ __global__ __launch_bounds__(THREADS, W == 4 ? 1 : 2) void k_linear(LinearProble
     });
   };
   auto round = [&]() CANZ_INLINE {
-    step(Zero{}, Zero{}, st0, st0);
-    step(One{}, Zero{}, st0, st1);
-    step(Zero{}, One{}, st1, st1);
-    step(One{}, One{}, st1, st0);
+    static_for<STAGES>([&](auto stage) CANZ_INLINE {
+      step(Zero{}, stage);
+      step(One{}, stage);
+    });
   };
 
   // Accumulator register r of lane l in tile (i, j) is row 16 i + l % 16, column 16 j + 4 (l / 16) + r of the wavefront's part.  Pieces of 32 x CW of it go through LDS, 16-byte
@@ -308,7 +318,8 @@ __global__ __launch_bounds__(THREADS, W == 4 ? 1 : 2) void k_linear(LinearProble
     const int64_t m = ps->pr[t.problem].m, n = ps->pr[t.problem].n;
     constexpr int CHUNKS = CW / 4, COLS = CW / 8, ROWS = 64 / COLS;   // of a row; lanes along a row, rows at a time
     float* const mine = turn[wave];
-    // One copy of what is done to a piece: a copy for each, 100 KB of instructions that a tile goes through once, took 15 us a tile, most of it waiting for them.
+    // One copy of what is done to a piece, to its four or eight rows at once: 4096 x 4096 x 256 takes 18.6 us, with a copy for each piece (100 KB of instructions) and its rows one after
+    // another 24.9.
 #pragma clang loop unroll(disable)
     for (int piece = 0; piece < 2 * W; ++piece) {
       static_for<2 * W>([&](auto x) CANZ_INLINE {
@@ -345,9 +356,10 @@ __global__ __launch_bounds__(THREADS, W == 4 ? 1 : 2) void k_linear(LinearProble
 
   load_next_tile();
   if (next_tile.problem < 0) return;   // this XCD's share is one tile less than others'
-  static_for<LOADS>([&](auto idx) CANZ_INLINE { fetch_one(Zero{}, st0, idx); });
-  static_for<LOADS>([&](auto idx) CANZ_INLINE { fetch_one(One{}, st1, idx); });
-  __builtin_amdgcn_s_waitcnt(wait_code(LOADS));
+  static_for<STAGES>([&](auto stage) CANZ_INLINE {
+    static_for<LOADS>([&](auto idx) CANZ_INLINE { fetch_one(stage, stage_at(stage), idx); });
+  });
+  __builtin_amdgcn_s_waitcnt(wait_code((STAGES - 1) * LOADS));
   __builtin_amdgcn_s_barrier();
   CANZ_FENCE();
   static_for<T>([&](auto idx) CANZ_INLINE {
@@ -367,8 +379,8 @@ __global__ __launch_bounds__(THREADS, W == 4 ? 1 : 2) void k_linear(LinearProble
         if constexpr (W == 4) asm volatile("" : "+a"(acc[i][j]));   // zeros that the compiler does not know: it would make them anew where a tile has but one round
       }
     // the last round, which loads the next tile's first one, apart: with both in one loop, what the loads need is copied to and fro in every round
-    for (int rounds = (ps->pr[t.problem].steps + 3) / 4; rounds > 1; --rounds) {
-      sa.next_round(), sb.next_round();
+    for (int rounds = (ps->pr[t.problem].steps + 2 * STAGES - 1) / (2 * STAGES); rounds > 1; --rounds) {
+      sa.template next_round<STAGES>(), sb.template next_round<STAGES>();
       round();
       settle<W == 4>();
     }
@@ -400,25 +412,32 @@ int longest_share(const LinearProblems& ps) {
 // Blocks for `each` tiles on every XCD, `most` (a multiple of 8) at a time.
 dim3 tile_grid(int64_t each, int most) { return dim3(static_cast<unsigned>(std::min<int64_t>(N_XCD * each, most))); }
 
-template <int W, bool MASK>
+template <int W, int STAGES, bool MASK>
 void launch(const LinearProblems& ps, bool at, bool bt, dim3 grid, hipStream_t st) {
   if (at && bt)
-    k_linear<W, true, true, false><<<grid, THREADS, 0, st>>>(ps);
+    k_linear<W, STAGES, true, true, false><<<grid, THREADS, 0, st>>>(ps);
   else if (at)
-    k_linear<W, true, false, MASK><<<grid, THREADS, 0, st>>>(ps);
+    k_linear<W, STAGES, true, false, MASK><<<grid, THREADS, 0, st>>>(ps);
   else if (bt)
-    k_linear<W, false, true, MASK><<<grid, THREADS, 0, st>>>(ps);
+    k_linear<W, STAGES, false, true, MASK><<<grid, THREADS, 0, st>>>(ps);
   else
-    k_linear<W, false, false, MASK><<<grid, THREADS, 0, st>>>(ps);
+    k_linear<W, STAGES, false, false, MASK><<<grid, THREADS, 0, st>>>(ps);
 }
-template <int W>
+template <int W, int STAGES>
 void launch(const LinearProblems& ps, bool at, bool bt, dim3 grid, hipStream_t st) {
   bool mask = false;
   for (int i = 0; i < ps.n; ++i) mask = mask || (!at && ps.pr[i].k_a % STAGE_K != 0) || (!bt && ps.pr[i].k_b % STAGE_K != 0);
   if (mask)
-    launch<W, true>(ps, at, bt, grid, st);
+    launch<W, STAGES, true>(ps, at, bt, grid, st);
   else
-    launch<W, false>(ps, at, bt, grid, st);
+    launch<W, STAGES, false>(ps, at, bt, grid, st);
+}
+// `each` small tiles on every XCD
+void launch_small(const LinearProblems& ps, int64_t each, bool at, bool bt, hipStream_t st) {
+  if (N_XCD * each <= LINEAR_CU)
+    launch<2, 4>(ps, at, bt, tile_grid(each, LINEAR_CU), st);
+  else
+    launch<2, 2>(ps, at, bt, tile_grid(each, 2 * LINEAR_CU), st);
 }
 
 }  // namespace
@@ -431,16 +450,16 @@ hipError_t launch_linear_tiles(LinearProblems& ps, bool a_trans, bool b_trans, h
   steps = (steps + small - 1) / small;
   ps.from = 0, ps.to = longest_share(ps), ps.quarters = 0;
   if (!linear_large_tiles(large, small, steps)) {
-    launch<2>(ps, a_trans, b_trans, tile_grid(ps.to, 2 * LINEAR_CU), st);
+    launch_small(ps, ps.to, a_trans, b_trans, st);
     return hipGetLastError();
   }
   count_tiles(ps, 256);
   const int all = longest_share(ps), whole = static_cast<int>(linear_whole_rounds(large, steps)) * (LINEAR_CU / N_XCD);
   ps.to = whole > 0 ? std::min(whole, all) : all;
-  launch<4>(ps, a_trans, b_trans, tile_grid(ps.to, LINEAR_CU), st);
+  launch<4, 2>(ps, a_trans, b_trans, tile_grid(ps.to, LINEAR_CU), st);
   if (ps.to < all) {   // what the last round would leave most CUs without
     ps.from = ps.to, ps.to = all, ps.quarters = 1;
-    launch<2>(ps, a_trans, b_trans, tile_grid(4 * (ps.to - ps.from), 2 * LINEAR_CU), st);
+    launch_small(ps, int64_t{4} * (ps.to - ps.from), a_trans, b_trans, st);
   }
   return hipGetLastError();
 }

@@ -12,6 +12,8 @@ extern "C" {
 int few(long long m, int a_trans, int b_trans) { return canz::linear_few(m, a_trans, b_trans); }
 int parts(long long m, long long n, long long k) { return canz::linear_parts(m, n, k); }
 int large_tiles(long long large, long long small, long long steps) { return canz::linear_large_tiles(large, small, steps); }
+long long whole_rounds(long long large, long long steps) { return canz::linear_whole_rounds(large, steps); }
+int cus() { return canz::LINEAR_CU; }
 }
 """
 
@@ -26,6 +28,7 @@ def lib():
         r = ctypes.CDLL(out)
     r.few.argtypes = [ctypes.c_longlong, ctypes.c_int, ctypes.c_int]
     r.parts.argtypes = r.large_tiles.argtypes = [ctypes.c_longlong] * 3
+    r.whole_rounds.argtypes, r.whole_rounds.restype = [ctypes.c_longlong] * 2, ctypes.c_longlong
     return r
 
 
@@ -37,9 +40,23 @@ def parts(m, n, k):
     return lib().parts(m, n, k)
 
 
-def large_tiles(m, n, k):
-    """Whether a product that is alone in its call (and not one of few rows) takes tiles of 256 x 256."""
+def _tiles(m, n, k):
     p = parts(m, n, k)
     large, small = p * (-(-m // 256) * -(-n // 256)), p * (-(-m // 128) * -(-n // 128))
-    steps = -(-k // 32)
-    return bool(lib().large_tiles(large, small, -(-(steps * (small // p)) // small)))
+    return large, small, -(-(-(-k // 32) * (small // p)) // small)
+
+
+def large_tiles(m, n, k):
+    """Whether a product that is alone in its call (and not one of few rows) takes tiles of 256 x 256."""
+    return bool(lib().large_tiles(*_tiles(m, n, k)))
+
+
+def quarters(m, n, k):
+    """How many of its 256 x 256 tiles are done in quarters by small ones behind the last whole round."""
+    large, _, steps = _tiles(m, n, k)
+    rounds = lib().whole_rounds(large, steps) if large_tiles(m, n, k) else 0
+    return large - rounds * lib().cus() if rounds else 0
+
+
+def one_small_tile_to_a_cu(m, n, k):
+    return not large_tiles(m, n, k) and -(-_tiles(m, n, k)[1] // 8) * 8 <= lib().cus()

@@ -94,14 +94,18 @@ class Product:
 FEW = [(1, 1, 1), (1, 33, 100), (2, 64, 128), (1, 1000, 4000), (16, 100, 640), (17, 64, 256), (31, 500, 77), (33, 129, 300), (64, 64, 1024), (5, 40, 9000), (3, 257, 1025), (64, 300, 129)]
 SMALL = [(65, 130, 129), (100, 1, 50), (1, 65, 8), (7, 9, 3), (128, 256, 512), (255, 257, 384), (257, 300, 1000), (500, 700, 1048), (640, 304, 128), (72, 8, 1), (130, 1000, 31)]
 LARGE = [(4096, 4096, 64), (2560, 6400, 104), (4090, 4095, 33)]
+TWO_TO_A_CU = [(1900, 3999, 100), (2048, 4000, 296)]
+QUARTERS = [(4200, 4400, 392), (4097, 4104, 776)]
 PARTS = [(65, 100, 16000), (128, 128, 8192), (200, 300, 9001), (513, 400, 7000), (100, 1000, 20000)]
 ORIENTATIONS = [(False, False), (False, True), (True, False), (True, True)]
 
 
 def test_shapes_reach_their_kernels():
     assert all(R.few(m) for m, _, _ in FEW) and not any(R.few(m, *t) for m, _, _ in FEW for t in ORIENTATIONS[1:])
-    assert all(R.parts(*s) == 1 and not R.large_tiles(*s) for s in SMALL)
-    assert all(R.parts(*s) == 1 and R.large_tiles(*s) for s in LARGE)
+    assert all(R.parts(*s) == 1 and R.one_small_tile_to_a_cu(*s) for s in SMALL)
+    assert all(R.parts(*s) == 1 and not R.large_tiles(*s) and not R.one_small_tile_to_a_cu(*s) for s in TWO_TO_A_CU)
+    assert all(R.parts(*s) == 1 and R.large_tiles(*s) and not R.quarters(*s) for s in LARGE)
+    assert all(R.parts(*s) == 1 and R.quarters(*s) > 0 for s in QUARTERS)
     assert all(R.parts(*s) > 1 for s in PARTS)
 
 
@@ -132,7 +136,7 @@ def test_small_tiles(canz, m, n, k, a_trans, b_trans):
 
 
 @pytest.mark.parametrize("a_trans,b_trans", ORIENTATIONS)
-@pytest.mark.parametrize("m,n,k", LARGE)
+@pytest.mark.parametrize("m,n,k", LARGE + QUARTERS + TWO_TO_A_CU)
 def test_large_tiles(canz, m, n, k, a_trans, b_trans):
     rng = np.random.default_rng(m + n + k)
     for out, odd in ((BF16, False), (F32, m % 8 != 0)):
