@@ -20,7 +20,7 @@ struct Forward {
 
 template <typename E, int ACT, bool UP>
 __global__ __launch_bounds__(EACH_THREADS) void k_act_forward(Forward a) {
-  const Spot s = spot(a.log_tx, a.across, FORWARD_ROWS);
+  const Spot s = spot(blockIdx.x, a.log_tx, a.across, FORWARD_ROWS);
   Raw<E> gate[FORWARD_ROWS], up[FORWARD_ROWS];
 #pragma unroll
   for (int i = 0; i < FORWARD_ROWS; ++i) {
@@ -67,7 +67,7 @@ struct Backward {
 template <typename E, typename I, int ACT, bool UP>
 __global__ __launch_bounds__(EACH_THREADS) void k_act_backward(Backward a) {
   constexpr bool IMAGE = std::is_same_v<I, Image8>;
-  const Spot s = spot(a.log_tx, a.across, BACKWARD_ROWS);
+  const Spot s = spot(blockIdx.x, a.log_tx, a.across, BACKWARD_ROWS);
   std::conditional_t<IMAGE, RawCodes, Raw<std::conditional_t<IMAGE, float, I>>> gate[BACKWARD_ROWS], up[BACKWARD_ROWS];
   Raw<E> dout[BACKWARD_ROWS];
 #pragma unroll

@@ -42,10 +42,22 @@ struct LinearProblems {
 
 // tiles: all problems of one launch have the same orientations
 hipError_t launch_linear_tiles(LinearProblems& ps, bool a_trans, bool b_trans, hipStream_t st);
-// up to LINEAR_FEW rows, both operands contiguous along k, at any address; the same kind of A in all of them
+// up to LINEAR_FEW rows, both operands contiguous along k, at any address; the same kind of A and of linear_few_wide in all of them
 hipError_t launch_linear_few(LinearProblems& ps, hipStream_t st);
-// C from the sum of `parts` matrices of m x pitch fp32 sums, one behind the other (none: from zeros)
-hipError_t launch_linear_join(const LinearProblem& p, const float* sums, int64_t pitch, int parts, hipStream_t st);
+// C from the sum of `parts` matrices of m x pitch fp32 sums, one behind the other (none: from zeros).
+struct LinearJoin {
+  LinearEnd end;
+  int64_t m, n, pitch;
+  const float* sums;
+  int parts, log_tx, across;
+};
+constexpr int LINEAR_JOINS = 16;
+struct LinearJoins {
+  int n;
+  unsigned first_block[LINEAR_JOINS + 1];
+  LinearJoin jn[LINEAR_JOINS];
+};
+hipError_t launch_linear_joins(LinearJoins& js, hipStream_t st);
 
 // A matrix as an operand of the tile kernels: bf16, rows `pitch` apart, zeros behind `cols`.
 struct LinearCopy {
@@ -78,8 +90,8 @@ hipError_t launch_linear_sums(const LinearSums& s, hipStream_t st);
 #if defined(__HIPCC__)
 // A kernel's argument where it lies: scalar loads at any index, and no copy of it.
 typedef const __attribute__((address_space(4))) LinearProblems* LinearArgs;
-__device__ __forceinline__ LinearEnd linear_end_of(LinearArgs ps, int j) {
-  const auto& e = ps->pr[j].end;
+template <typename E>   // a LinearEnd among a kernel's arguments
+__device__ __forceinline__ LinearEnd linear_end_of(const E& e) {
   return LinearEnd{e.c, e.r, e.bias, Image8{e.pre.codes, e.pre.scales, e.pre.pitch}, e.ldc, e.ldr, e.alpha, e.beta, e.act, e.out_f32, e.bias_f32};
 }
 

@@ -33,24 +33,29 @@ __global__ __launch_bounds__(EACH_THREADS) void k_linear_copy(LinearCopies) {
 }
 
 // ---- sums of parts of k ---------------------------------------------------------------------------------------------------------
+typedef const __attribute__((address_space(4))) LinearJoins* JoinArgs;
+
 // A thread has eight columns of a row, its quad a block of 32; pieces beyond the padded row fill up the last block of threads.
-__global__ __launch_bounds__(EACH_THREADS) void k_linear_join(LinearEnd e, int64_t m, int64_t n, const float* sums, int64_t pitch, int parts, int log_tx, int across) {
-  const Spot s = spot(log_tx, across, 1);
-  const int64_t part_elements = m * pitch;
-  const bool there = s.row < m;
-  f32x8 v = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  if (there && s.col < pitch) {
-    const float* const p = sums + s.row * pitch + s.col;
+__global__ __launch_bounds__(EACH_THREADS) void k_linear_join(LinearJoins) {
+  const JoinArgs js = (JoinArgs)__builtin_amdgcn_kernarg_segment_ptr();
+  int j = 0;
+  while (blockIdx.x >= js->first_block[j + 1]) ++j;
+  const auto& q = js->jn[j];
+  const Spot s = spot(blockIdx.x - js->first_block[j], q.log_tx, q.across, 1);
+  const int64_t part_elements = q.m * q.pitch;
+  const int parts = q.parts;
+  f32x8 z[1] = {f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
+  if (s.row < q.m && s.col < q.pitch) {
+    const float* const p = q.sums + s.row * q.pitch + s.col;
     Raw<float> part[LINEAR_MAX_PARTS];
 #pragma unroll
-    for (int q = 0; q < LINEAR_MAX_PARTS; ++q)
-      if (q < parts) part[q] = load_raw(p + q * part_elements, PIECE);   // all on their way before the first is added
+    for (int i = 0; i < LINEAR_MAX_PARTS; ++i)
+      if (i < parts) part[i] = load_raw(p + i * part_elements, PIECE);   // all on their way before the first is added
 #pragma unroll
-    for (int q = 0; q < LINEAR_MAX_PARTS; ++q)
-      if (q < parts) v += part[q].v;
+    for (int i = 0; i < LINEAR_MAX_PARTS; ++i)
+      if (i < parts) z[0] += part[i].v;
   }
-  f32x8 z[1] = {v};
-  linear_end<false, 1>(e, s.row, 0, s.col, m, n, z);
+  linear_end<false, 1>(linear_end_of(q.end), s.row, 0, s.col, q.m, q.n, z);
 }
 
 // ---- sums of A's rows -----------------------------------------------------------------------------------------------------------
@@ -122,9 +127,16 @@ hipError_t launch_linear_copies(LinearCopies& cs, hipStream_t st) {
   return hipGetLastError();
 }
 
-hipError_t launch_linear_join(const LinearProblem& p, const float* sums, int64_t pitch, int parts, hipStream_t st) {
-  const Cover c = cover(p.m, p.n, 1);
-  k_linear_join<<<dim3(static_cast<unsigned>(c.blocks)), EACH_THREADS, 0, st>>>(p.end, p.m, p.n, sums, pitch, parts, c.log_tx, c.across);
+hipError_t launch_linear_joins(LinearJoins& js, hipStream_t st) {
+  int64_t blocks = 0;
+  for (int i = 0; i < js.n; ++i) {
+    const Cover c = cover(js.jn[i].m, js.jn[i].n, 1);
+    js.jn[i].log_tx = c.log_tx, js.jn[i].across = c.across;
+    js.first_block[i] = static_cast<unsigned>(blocks);
+    blocks += c.blocks;
+  }
+  js.first_block[js.n] = static_cast<unsigned>(blocks);
+  k_linear_join<<<dim3(static_cast<unsigned>(blocks)), EACH_THREADS, 0, st>>>(js);
   return hipGetLastError();
 }
 

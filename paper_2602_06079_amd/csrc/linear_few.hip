@@ -4,6 +4,7 @@
 // 8-bit image whose elements the lane that needs them turns into bf16) come out of L2.  Memory is all that takes time: each wavefront keeps AHEAD units in flight.
 //
 // v_mfma_f32_16x16x32_bf16 with B first: lane l supplies 8 k (from 8 (l / 16) on) of row l % 16 of either, and holds columns 4 (l / 16) .. + 3 of row l % 16 of C.
+#include <algorithm>
 #include <type_traits>
 
 #include "linear.h"
@@ -15,6 +16,7 @@ namespace {
 #define CANZ_FENCE() __builtin_amdgcn_sched_barrier(0)
 
 constexpr int UNIT = 128, PARTS = UNIT / 32;   // k of a unit, instructions for it
+constexpr int WAVES = 4;                       // of a block
 
 // Eight k of a row of A on their way from memory.
 template <bool IMAGE>
@@ -34,7 +36,7 @@ __device__ __forceinline__ bf16x8 operand(const RawA<true>& r, unsigned scale) {
   return o;
 }
 
-template <bool IMAGE, int UM, int UN, int WAVES, int AHEAD>
+template <bool IMAGE, int UM, int UN, int AHEAD>
 __global__ __launch_bounds__(64 * WAVES) void k_linear_few(LinearProblems) {
   const LinearArgs ps = (LinearArgs)__builtin_amdgcn_kernarg_segment_ptr();
   __shared__ f32x4 sums[WAVES][UM * UN][64];
@@ -145,7 +147,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_linear_few(LinearProblems) {
     for (int q = 0; q < UN; ++q) sums[wave][i * UN + q][lane] = acc[i][q];
   __syncthreads();
   // eight columns of a row per thread: columns 8 c .. of the block's 16 UN lie in tile c / 2, lanes from 32 (c % 2) on
-  const LinearEnd e = linear_end_of(ps, j);
+  const LinearEnd e = linear_end_of(ps->pr[j].end);
   constexpr int COLS = 2 * UN;
   for (int x = threadIdx.x; x < 16 * UM * COLS; x += 64 * WAVES) {
     const int c = x % COLS, row = x / COLS, tile = row / 16 * UN + c / 2, from = (c & 1) * 32 + (row & 15);
@@ -157,7 +159,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_linear_few(LinearProblems) {
   }
 }
 
-template <bool IMAGE, int UM, int UN, int WAVES, int AHEAD>
+template <bool IMAGE, int UM, int UN, int AHEAD>
 void launch(LinearProblems& ps, hipStream_t st) {
   int64_t blocks = 0;
   for (int i = 0; i < ps.n; ++i) {
@@ -166,18 +168,31 @@ void launch(LinearProblems& ps, hipStream_t st) {
     blocks += (cols + 16 * UN - 1) / (16 * UN);
   }
   ps.first_tile[ps.n] = static_cast<int>(blocks);
-  k_linear_few<IMAGE, UM, UN, WAVES, AHEAD><<<dim3(static_cast<unsigned>(blocks)), 64 * WAVES, 0, st>>>(ps);
+  k_linear_few<IMAGE, UM, UN, AHEAD><<<dim3(static_cast<unsigned>(blocks)), 64 * WAVES, 0, st>>>(ps);
 }
 
+// The wavefronts alone decide the order of a sum, so products of different numbers of rows may share a launch.  us, 64 rows of B to a block / 32 / 32 and eight wavefronts: 1 x 25600 x 5120
+// 52 / 53 / 56 (262 MB, 5.0 TB/s), 17 x 25600 x 5120 60 / 69 / 78, 16 x 12288 x 4096 24 / 32 / 30, 64 x 12288 x 4096 35 / 49 / 50; 1 x 5120 x 25600 97 / 56 / 57, 8 x 4096 x 4096 20 / 14 / 13,
+// 37 x 1536 x 4096 28 / 21 / 20, 1 x 1024 x 1024 7.3 / 5.1 / 7.7.
 template <bool IMAGE>
 void launch(LinearProblems& ps, hipStream_t st) {
-  const int64_t m = ps.pr[0].m;
-  if (m <= 16)
-    launch<IMAGE, 1, 2, 8, 2>(ps, st);
-  else if (m <= 32)
-    launch<IMAGE, 2, 2, 8, 2>(ps, st);
-  else
-    launch<IMAGE, 4, 2, 8, 1>(ps, st);
+  int64_t m = 0;
+  for (int i = 0; i < ps.n; ++i) m = std::max(m, ps.pr[i].m);
+  if (linear_few_wide(ps.pr[0].n)) {
+    if (m <= 16)
+      launch<IMAGE, 1, 4, 2>(ps, st);
+    else if (m <= 32)
+      launch<IMAGE, 2, 4, 2>(ps, st);
+    else
+      launch<IMAGE, 4, 4, 1>(ps, st);
+  } else {
+    if (m <= 16)
+      launch<IMAGE, 1, 2, 2>(ps, st);
+    else if (m <= 32)
+      launch<IMAGE, 2, 2, 2>(ps, st);
+    else
+      launch<IMAGE, 4, 2, 1>(ps, st);
+  }
 }
 
 }  // namespace

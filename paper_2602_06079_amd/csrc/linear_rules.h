@@ -13,6 +13,7 @@ constexpr int LINEAR_ROUND = 128;   // k of a round of a ring of two stages
 // The kernel for few rows takes up to this many rows of A, where both operands are contiguous along k.
 constexpr int LINEAR_FEW = 64;
 constexpr bool linear_few(int64_t m, bool a_trans, bool b_trans) { return m <= LINEAR_FEW && !a_trans && !b_trans; }
+constexpr bool linear_few_wide(int64_t n) { return n >= 12288; }   // blocks of 64 rows of B instead of 32 (figures at the kernel)
 
 // ns that a launch takes by the tiles it has, for `steps` of 32 k.  256 x 256 in rounds of one to a CU, of which beginning and end are not hidden; 128 x 128 one to a CU with a ring of four
 // stages, or two to a CU with two.  us measured (large; small): 4096 x 4096 x 256 18; 19, x 1024 34; 39, x 4096 99; 117; 8192 x 4096 x 512 42; 48; 2048 x 4096 x 1024 35; 21, x 4096 88; 60; 1024 x 4096 x

@@ -111,44 +111,38 @@ int workspace_of(const canz_linear_group* g, int32_t n_groups, size_t* bytes_out
 }
 
 // The launches that a product may be part of.
-enum Kind { JOIN, TILES, FEW = TILES + 4, KINDS = FEW + 6 };
+enum Kind { JOIN, TILES, FEW = TILES + 4, KINDS = FEW + 4 };
 int kind_of(const canz_linear_group& g) {
   if (g.k == 0) return JOIN;
   if (!runs_few(g)) return TILES + 2 * g.a_trans + g.b_trans;
-  return FEW + (g.a_dtype == CANZ_DT_MX8 ? 3 : 0) + (g.m <= 16 ? 0 : g.m <= 32 ? 1 : 2);
+  return FEW + (g.a_dtype == CANZ_DT_MX8 ? 2 : 0) + linear_few_wide(g.n);
 }
 
 int hip_failed(hipError_t err) { return err == hipSuccess ? CANZ_OK : fail(CANZ_EHIP, "linear: %s", hipGetErrorString(err)); }
-
-struct Join {
-  LinearProblem p;
-  const float* sums;
-  int64_t pitch;
-  int parts;
-};
 
 // Problems wait here until their launch is full.
 class Launches {
  public:
   explicit Launches(hipStream_t st) : st_(st) {
     for (auto& ps : waiting_) ps.n = 0;
+    joins_.n = 0;
   }
   int add(int kind, const LinearProblem& p) {
     LinearProblems& ps = waiting_[kind];
     ps.pr[ps.n++] = p;
     return ps.n == LINEAR_PROBLEMS ? flush(kind) : CANZ_OK;
   }
-  int join(const Join& j) {
-    joins_[n_joins_++] = j;
-    return n_joins_ == JOINS ? flush() : CANZ_OK;
+  // behind the products that have been added
+  int join(const LinearProblem& p, const float* sums, int64_t pitch, int parts) {
+    joins_.jn[joins_.n++] = LinearJoin{p.end, p.m, p.n, pitch, sums, parts, 0, 0};
+    return joins_.n == LINEAR_JOINS ? flush() : CANZ_OK;
   }
   int flush() {
     for (int kind = 0; kind < KINDS; ++kind)
       if (int rc = flush(kind)) return rc;
-    for (int i = 0; i < n_joins_; ++i)
-      if (int rc = hip_failed(launch_linear_join(joins_[i].p, joins_[i].sums, joins_[i].pitch, joins_[i].parts, st_))) return rc;
-    n_joins_ = 0;
-    return CANZ_OK;
+    const int rc = joins_.n > 0 ? hip_failed(launch_linear_joins(joins_, st_)) : CANZ_OK;
+    joins_.n = 0;
+    return rc;
   }
 
  private:
@@ -159,11 +153,9 @@ class Launches {
     ps.n = 0;
     return hip_failed(err);
   }
-  static constexpr int JOINS = 16;
   hipStream_t st_;
   LinearProblems waiting_[KINDS];
-  Join joins_[JOINS];
-  int n_joins_ = 0;
+  LinearJoins joins_;
 };
 
 int run(const canz_linear_group* g, int32_t n_groups, uint8_t* ws, hipStream_t st) {
@@ -214,7 +206,7 @@ int run(const canz_linear_group* g, int32_t n_groups, uint8_t* ws, hipStream_t s
       p.end = LinearEnd{x.c[q], x.residual ? x.residual[q] : x.c[q], x.bias ? x.bias[q] : nullptr, image8(x.pre8 ? x.pre8[q] : nullptr, x.m, x.n), x.ldc,
                         x.residual ? x.ldr : x.ldc, x.alpha, x.beta, x.act, x.out_dtype == CANZ_DT_F32, x.bias_dtype == CANZ_DT_F32};
       if (x.k == 0) {
-        if (int rc = launches.join(Join{p, nullptr, sum_pitch(x.n), 0})) return rc;
+        if (int rc = launches.join(p, nullptr, sum_pitch(x.n), 0)) return rc;
         continue;
       }
       const bool few = runs_few(x);
@@ -247,7 +239,7 @@ int run(const canz_linear_group* g, int32_t n_groups, uint8_t* ws, hipStream_t s
         part.end = LinearEnd{sums + z * x.m * pitch, nullptr, nullptr, Image8{nullptr, nullptr, 0}, pitch, pitch, 1.f, 0.f, CANZ_ACT_NONE, 1, 1};
         if (int rc = launches.add(kind, part)) return rc;
       }
-      if (int rc = launches.join(Join{p, sums, pitch, parts})) return rc;
+      if (int rc = launches.join(p, sums, pitch, parts)) return rc;
     }
   }
   return launches.flush();

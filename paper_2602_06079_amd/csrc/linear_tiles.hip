@@ -314,7 +314,7 @@ __global__ __launch_bounds__(THREADS, W == 2 && STAGES == 2 ? 2 : 1) void k_line
   auto store_tile = [&](const Tile& t) CANZ_INLINE {
     int l = threadIdx.x & 63;   // opaque, or every address that depends on it is kept across the tiles
     asm volatile("" : "+v"(l));
-    const LinearEnd e = linear_end_of(ps, t.problem);
+    const LinearEnd e = linear_end_of(ps->pr[t.problem].end);
     const int64_t m = ps->pr[t.problem].m, n = ps->pr[t.problem].n;
     constexpr int CHUNKS = CW / 4, COLS = CW / 8, ROWS = 64 / COLS;   // of a row; lanes along a row, rows at a time
     float* const mine = turn[wave];

@@ -173,8 +173,8 @@ struct Spot {
   int64_t row, col;
   int step;   // rows from one of the thread's rows to the next
 };
-__device__ __forceinline__ Spot spot(int log_tx, int across, int rows_a_thread) {
-  const unsigned down = blockIdx.x / static_cast<unsigned>(across), along = blockIdx.x - down * across;
+__device__ __forceinline__ Spot spot(unsigned block, int log_tx, int across, int rows_a_thread) {
+  const unsigned down = block / static_cast<unsigned>(across), along = block - down * across;
   const int ty = threadIdx.x >> log_tx, tx = threadIdx.x & ((1 << log_tx) - 1), high = EACH_THREADS >> log_tx;
   return Spot{static_cast<int64_t>(down) * high * rows_a_thread + ty, ((static_cast<int64_t>(along) << log_tx) + tx) * PIECE, high};
 }

@@ -17,7 +17,7 @@ constexpr int ROWS_EACH = 4;   // rows of a thread, all of their loads in flight
 
 template <typename E>
 __global__ __launch_bounds__(EACH_THREADS) void k_mx8_store(const E* mat, int64_t ld, Image8 image, int64_t rows, int64_t cols, int log_tx, int across) {
-  const Spot s = spot(log_tx, across, ROWS_EACH);
+  const Spot s = spot(blockIdx.x, log_tx, across, ROWS_EACH);
   Raw<E> v[ROWS_EACH];
 #pragma unroll
   for (int i = 0; i < ROWS_EACH; ++i) {
@@ -34,7 +34,7 @@ __global__ __launch_bounds__(EACH_THREADS) void k_mx8_store(const E* mat, int64_
 
 template <typename E>
 __global__ __launch_bounds__(EACH_THREADS) void k_mx8_load(E* mat, int64_t ld, Image8 image, int64_t rows, int64_t cols, int log_tx, int across) {
-  const Spot s = spot(log_tx, across, ROWS_EACH);
+  const Spot s = spot(blockIdx.x, log_tx, across, ROWS_EACH);
   RawCodes v[ROWS_EACH];
 #pragma unroll
   for (int i = 0; i < ROWS_EACH; ++i) {
