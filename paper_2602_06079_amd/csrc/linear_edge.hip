@@ -80,16 +80,28 @@ __global__ __launch_bounds__(EACH_THREADS) void k_linear_row_sums(LinearSums a) 
   if ((threadIdx.x & 63) == 0) a.sums[row] = a.beta != 0.f ? __builtin_fmaf(a.beta, a.sums[row], a.alpha * t) : a.alpha * t;
 }
 
-// Across k: a block has 512 columns (64 pieces) of a group of rows, of which its four wavefronts take one each by turns; the groups' sums are added up by k_linear_join_sums.
+// Across k: a block has 512 columns (64 pieces) of a group of rows, of which its four wavefronts take one each by turns, eight of them on their way at a time; the groups' sums are added up by
+// k_linear_join_sums.
 __global__ __launch_bounds__(EACH_THREADS) void k_linear_column_sums(LinearSums a, int across) {
   __shared__ f32x8 part[3][64];
   const unsigned group = blockIdx.x / static_cast<unsigned>(across), along = blockIdx.x - group * across;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t groups = linear_sum_groups(a.rows), col = (static_cast<int64_t>(along) * 64 + lane) * PIECE;
+  const int64_t groups = linear_sum_groups(a.rows), col = (static_cast<int64_t>(along) * 64 + lane) * PIECE, step = 4 * groups;
   f32x8 s = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   if (col < a.cols) {
-#pragma unroll 4
-    for (int64_t row = group + wave * groups; row < a.rows; row += 4 * groups) s += piece_of(a, row, col);
+    int64_t row = group + wave * groups;
+    if (!a.scales && col + PIECE <= a.cols) {
+      constexpr int AHEAD = 8;
+      const __bf16* p = static_cast<const __bf16*>(a.from) + row * a.ld + col;
+      for (; row + (AHEAD - 1) * step < a.rows; row += AHEAD * step, p += AHEAD * step * a.ld) {
+        Raw<__bf16> v[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) v[i] = load_raw(p + i * step * a.ld, PIECE);
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) s += widen(v[i]);
+      }
+    }
+    for (; row < a.rows; row += step) s += piece_of(a, row, col);
   }
   if (wave > 0) part[wave - 1][lane] = s;
   __syncthreads();
@@ -103,8 +115,10 @@ __global__ __launch_bounds__(JOIN * 8) void k_linear_join_sums(LinearSums a) {
   const int tx = threadIdx.x & (JOIN - 1), ty = threadIdx.x / JOIN;
   const int64_t col = static_cast<int64_t>(blockIdx.x) * JOIN + tx, groups = linear_sum_groups(a.rows), pitch = mx8_pitch(a.cols);
   float s = 0.f;
-  if (col < a.cols)
+  if (col < a.cols) {
+#pragma unroll 8
     for (int64_t g = ty; g < groups; g += 8) s += a.partial[g * pitch + col];
+  }
   part[ty][tx] = s;
   __syncthreads();
   if (ty != 0 || col >= a.cols) return;

@@ -265,8 +265,10 @@ __global__ __launch_bounds__(JOIN * JOIN) void k_norm_join(const float* partial,
   const int tx = threadIdx.x & (JOIN - 1), ty = threadIdx.x / JOIN;
   const int64_t col = static_cast<int64_t>(blockIdx.x) * JOIN + tx;
   float s = 0.f;
-  if (col < cols)
+  if (col < cols) {
+#pragma unroll 8
     for (int64_t g = ty; g < groups; g += JOIN) s += partial[g * pitch + col];
+  }
   part[ty][tx] = s;
   __syncthreads();
   if (ty != 0 || col >= cols) return;
