@@ -188,6 +188,8 @@ int check_backward(const canz_act_grad& a, int idx) {
     return fail(CANZ_EINVAL, "activation %d: gate or up null or not aligned to %s", idx, in == 256 ? "256 bytes" : "its elements");
   if (bad(a.dout, el, a.dgate || a.dup) || bad(a.dgate, el, false) || bad(a.dup, el, false) || bad(a.out, el, false))
     return fail(CANZ_EINVAL, "activation %d: a matrix is null or not aligned to its elements", idx);
+  if (((a.dgate && a.dgate == a.gate) || (a.dup && a.dup == a.up)) && a.in_dtype != a.dtype)
+    return fail(CANZ_EINVAL, "activation %d: a gradient over its argument, which has another type", idx);
   return CANZ_OK;
 }
 

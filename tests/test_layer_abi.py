@@ -120,6 +120,8 @@ def test_act_refusals(canz):
     assert b(in_dtype=canz.DT_MX) == canz.EUNSUPPORTED
     assert b(dtype=canz.DT_MX8) == canz.EUNSUPPORTED
     assert b(act=9) == canz.EUNSUPPORTED
+    assert b(dgate=8192) == canz.EINVAL and "another type" in canz.canz_last_error()       # over an image
+    assert b(dup=12288, in_dtype=canz.DT_F32) == canz.EINVAL
     canz.canz_act_backward([], 0)
     canz.canz_act_backward([canz.ActGrad(rows=0, cols=7), canz.ActGrad(rows=7, cols=0)], 0)
 
