@@ -580,7 +580,7 @@ int canz_muon_step_images(const canz_group* g, int32_t n_groups, const canz_muon
  *
  * Conventions of all these calls.  Matrices are row-major in fp32 or bf16, at any address that is a multiple of their element's size; rows lie any number of elements
  * apart, at least their length, and what lies between them stays as it is.  8-bit images and workspaces are 256-byte aligned.  Extents are at
- * most 4194240 each, padded matrices (images: see below) at most 2^37 elements; an extent may be 0.  Tables and structures are the host's and are read
+ * most 4194240 each, matrices at most 2^34 elements with both extents padded to 128; an extent may be 0.  Tables and structures are the host's and are read
  * during the call.  The calls issue kernel launches only (no allocation, copy, memset or synchronisation), on the device hip_stream
  * belongs to (NULL, hipStreamLegacy and hipStreamPerThread: the current one), and may be recorded into a HIP graph.  What a call writes must not overlap any other buffer of
  * the call, but where it says so; what it only reads may be given any number of times.  Sums are formed in fp32 in an order that depends on extents
@@ -595,7 +595,7 @@ int canz_muon_step_images(const canz_group* g, int32_t n_groups, const canz_muon
  * (E4M3: a sign, 4 significant bits down to 2^-6, the spacing 2^-9 below, at most 448) as the value nearest to it, ties to the even code, times X: off by
  * at most 2^-4 of itself or 2^-10 X (magnitudes above 448 2^119 = 2.98e38 become that).  Every value is finite and exact in fp32 and in bf16.  A block that holds an infinity or a NaN is NaN as a
  * whole (byte 255, codes 0).  In memory: the codes row by row, rows padded to multiples of 128 bytes, then the scale bytes row by row, a
- * 32nd of that; padding is written as zeros with scale 0 and not looked at.  Images may be copied and sent as canz_mx_eight_bytes() bytes.
+ * 32nd of that; padding is written as zeros with scale 0, and has to be that in an image that comes from elsewhere.  Images may be copied and sent as canz_mx_eight_bytes() bytes.
  */
 
 /* Bytes of an 8-bit image of `rows` x `cols` elements (a multiple of 256; 0 if an extent is 0). */

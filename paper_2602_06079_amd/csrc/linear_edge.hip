@@ -132,26 +132,43 @@ __global__ __launch_bounds__(JOIN * 8) void k_linear_join_sums(LinearSums a) {
 
 hipError_t launch_linear_copies(LinearCopies& cs, hipStream_t st) {
   int64_t blocks = 0;
+  LinearCopies rest;
+  rest.n = 0;
   for (int i = 0; i < cs.n; ++i) {
+    const int64_t each = (cs.cp[i].rows + COPY_ROWS - 1) / COPY_ROWS * ((cs.cp[i].pitch + COPY_COLS - 1) / COPY_COLS);
+    if (blocks + each > MOST_BLOCKS) {
+      rest.n = cs.n - i, cs.n = i;
+      std::copy_n(cs.cp + i, rest.n, rest.cp);
+      break;
+    }
     cs.first_block[i] = static_cast<unsigned>(blocks);
-    blocks += (cs.cp[i].rows + COPY_ROWS - 1) / COPY_ROWS * ((cs.cp[i].pitch + COPY_COLS - 1) / COPY_COLS);
+    blocks += each;
   }
   cs.first_block[cs.n] = static_cast<unsigned>(blocks);
   k_linear_copy<<<dim3(static_cast<unsigned>(blocks)), EACH_THREADS, 0, st>>>(cs);
-  return hipGetLastError();
+  const hipError_t err = hipGetLastError();
+  return err == hipSuccess && rest.n > 0 ? launch_linear_copies(rest, st) : err;
 }
 
 hipError_t launch_linear_joins(LinearJoins& js, hipStream_t st) {
   int64_t blocks = 0;
+  LinearJoins rest;
+  rest.n = 0;
   for (int i = 0; i < js.n; ++i) {
     const Cover c = cover(js.jn[i].m, js.jn[i].n, 1);
+    if (blocks + c.blocks > MOST_BLOCKS) {
+      rest.n = js.n - i, js.n = i;
+      std::copy_n(js.jn + i, rest.n, rest.jn);
+      break;
+    }
     js.jn[i].log_tx = c.log_tx, js.jn[i].across = c.across;
     js.first_block[i] = static_cast<unsigned>(blocks);
     blocks += c.blocks;
   }
   js.first_block[js.n] = static_cast<unsigned>(blocks);
   k_linear_join<<<dim3(static_cast<unsigned>(blocks)), EACH_THREADS, 0, st>>>(js);
-  return hipGetLastError();
+  const hipError_t err = hipGetLastError();
+  return err == hipSuccess && rest.n > 0 ? launch_linear_joins(rest, st) : err;
 }
 
 hipError_t launch_linear_sums(const LinearSums& s, hipStream_t st) {

@@ -27,8 +27,8 @@ int check_group(const canz_linear_group& g, int idx, bool need_ptrs) {
   if (g.m < 0 || g.n < 0 || g.k < 0) return fail(CANZ_EINVAL, "group %d: negative extent", idx);
   if (g.m > LINEAR_MAX_EXTENT || g.n > LINEAR_MAX_EXTENT || g.k > LINEAR_MAX_EXTENT)
     return fail(CANZ_ESHAPE, "group %d: extent above %lld", idx, static_cast<long long>(LINEAR_MAX_EXTENT));
-  if (!mx_fits_grid(g.m, g.n) || !mx_fits_grid(g.m, g.k) || !mx_fits_grid(g.n, g.k))
-    return fail(CANZ_ESHAPE, "group %d: more than 2^37 padded elements in a matrix", idx);
+  if (!fits_launch(g.m, g.n) || !fits_launch(g.m, g.k) || !fits_launch(g.n, g.k))
+    return fail(CANZ_ESHAPE, "group %d: more than 2^34 padded elements in a matrix", idx);
   for (int32_t t : {g.a_dtype, g.b_dtype})
     if (t != CANZ_DT_BF16 && t != CANZ_DT_MX8) return fail(CANZ_EUNSUPPORTED, "group %d: an operand's dtype is neither CANZ_DT_BF16 nor CANZ_DT_MX8", idx);
   if (!float_dtype(g.out_dtype) || !float_dtype(g.bias_dtype)) return fail(CANZ_EUNSUPPORTED, "group %d: unknown out_dtype or bias_dtype", idx);

@@ -180,6 +180,9 @@ __device__ __forceinline__ Spot spot(unsigned block, int log_tx, int across, int
 }
 
 // Checks that the entry points share.
+// Elements of a matrix, padded to 128 either way: a launch has fewer than 2^32 threads, and a thread at least 8 elements.
+constexpr bool fits_launch(int64_t rows, int64_t cols) { return ((rows + 127) / 128) * ((cols + 127) / 128) <= (int64_t(1) << 34) / (128 * 128); }
+constexpr int64_t MOST_BLOCKS = (int64_t(1) << 24) - 1;   // of EACH_THREADS in a launch
 inline bool misaligned(const void* p, uintptr_t align) { return (reinterpret_cast<uintptr_t>(p) & (align - 1)) != 0; }
 constexpr bool float_dtype(int32_t t) { return t == CANZ_DT_F32 || t == CANZ_DT_BF16; }
 constexpr uintptr_t element_bytes(int32_t t) { return t == CANZ_DT_F32 ? 4 : 2; }

@@ -7,7 +7,7 @@ namespace canz {
 int check_extents(const char* what, int idx, int64_t rows, int64_t cols) {
   if (rows < 0 || cols < 0) return fail(CANZ_EINVAL, "%s %d: negative extent", what, idx);
   if (rows > MX_MAX_EXTENT || cols > MX_MAX_EXTENT) return fail(CANZ_ESHAPE, "%s %d: extent above %lld", what, idx, static_cast<long long>(MX_MAX_EXTENT));
-  if (!mx_fits_grid(rows, cols)) return fail(CANZ_ESHAPE, "%s %d: more than 2^37 padded elements in a matrix", what, idx);
+  if (!fits_launch(rows, cols)) return fail(CANZ_ESHAPE, "%s %d: more than 2^34 padded elements in a matrix", what, idx);
   return CANZ_OK;
 }
 

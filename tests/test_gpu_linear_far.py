@@ -89,3 +89,18 @@ def test_subnormal_operands(canz, m):
     c = torch.empty(m, n, device="cuda")
     call(canz, [canz.Linear(m=m, n=n, k=k, a=[a], b=[b], c=[c], out_dtype=F32)])
     assert (c.double().cpu().numpy() == 64 * 3 * 2.0 ** -110).all()
+
+
+def test_largest_matrices(canz):
+    """2^34 elements: two results without products (k = 0) in one call, more blocks than a launch has, then an activation over one of them."""
+    import torch
+    n = 131072
+    c = [torch.empty(n, n, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    bias = [torch.arange(n, device="cuda").remainder(251).float() - s for s in (100, 120)]
+    call(canz, [canz.Linear(m=n, n=n, k=0, a=[0, 0], b=[0, 0], c=c, bias=bias, act=L.NONE)])
+    rows = (0, 1, 32767, 65535, 65536, n - 1)
+    for x, v in zip(c, bias):
+        assert all(torch.equal(x[r].float(), v) for r in rows)
+    canz.canz_act_forward([canz.Act(rows=n, cols=n, gate=c[0], out=c[1], act=L.RELU)], stream())
+    torch.cuda.synchronize()
+    assert all(torch.equal(c[1][r].float(), bias[0].clamp(min=0)) for r in rows)

@@ -64,6 +64,8 @@ def test_images_refusals(canz):
         assert f(n_mats=-2, mat=[], image=[]) == canz.EINVAL
         assert f(rows=4194241) == canz.ESHAPE
         assert f(rows=4194240, cols=4194240) == canz.ESHAPE
+        assert f(rows=131073, cols=131072) == canz.ESHAPE and "2^34" in canz.canz_last_error()
+        assert f(rows=131072, cols=131072, mat=[0]) == canz.EINVAL
         assert f(dtype=canz.DT_MX) == canz.EUNSUPPORTED
         assert f(dtype=canz.DT_MX8) == canz.EUNSUPPORTED
         # a later group that is wrong stops the call before the first is enqueued (no device here: a launch would fail otherwise)
@@ -243,8 +245,11 @@ def test_linear_refusals_and_workspace(canz):
     assert "workspace too small" in canz.canz_last_error()
     assert w([]) == 256
     assert _code(canz, w, [P(m=1, n=1, k=-1, n_prods=1)]) == canz.EINVAL
-    many = dict(m=1 << 18, n=128, k=1 << 19, n_prods=(1 << 31) - 1)
-    assert _code(canz, w, [P(**many)]) == canz.ESHAPE
+    many = dict(m=1 << 17, n=128, k=1 << 17, n_prods=(1 << 31) - 1)
+    assert _code(canz, w, [P(**many)]) == canz.ESHAPE and "64 bits" in canz.canz_last_error()
+    for extents in (dict(m=131073, n=131072, k=1), dict(m=131073, n=1, k=131072), dict(m=1, n=131073, k=131072)):
+        assert _code(canz, w, [P(n_prods=1, **extents)]) == canz.ESHAPE and "2^34" in canz.canz_last_error()
+    assert w([P(m=131072, n=131072, k=0, n_prods=1)]) == 256
     # a later group that is wrong stops the call before the first is enqueued (no device here: a launch would fail otherwise)
     assert _code(canz, canz.canz_linear, [P(**ok), P(**{**ok, "ldc": 1})], 256 * 1024, 1 << 40, 0) == canz.EINVAL
     with pytest.raises(ValueError):
