@@ -42,7 +42,7 @@ struct LinearProblems {
 
 // tiles: all problems of one launch have the same orientations
 hipError_t launch_linear_tiles(LinearProblems& ps, bool a_trans, bool b_trans, hipStream_t st);
-// up to LINEAR_FEW rows, both operands contiguous along k, at any address; the same kind of A and of linear_few_wide in all of them
+// up to LINEAR_FEW rows, both operands contiguous along k, at any address; the same kind of A and the same linear_few_width in all of them
 hipError_t launch_linear_few(LinearProblems& ps, hipStream_t st);
 // C from the sum of `parts` matrices of m x pitch fp32 sums, one behind the other (none: from zeros).
 struct LinearJoin {

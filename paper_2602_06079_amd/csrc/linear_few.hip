@@ -173,25 +173,26 @@ void launch(LinearProblems& ps, hipStream_t st) {
 
 // The wavefronts alone decide the order of a sum, so products of different numbers of rows may share a launch.  us, 64 rows of B to a block / 32 / 32 and eight wavefronts: 1 x 25600 x 5120
 // 52 / 53 / 56 (262 MB, 5.0 TB/s), 17 x 25600 x 5120 60 / 69 / 78, 16 x 12288 x 4096 24 / 32 / 30, 64 x 12288 x 4096 35 / 49 / 50; 1 x 5120 x 25600 97 / 56 / 57, 8 x 4096 x 4096 20 / 14 / 13,
-// 37 x 1536 x 4096 28 / 21 / 20, 1 x 1024 x 1024 7.3 / 5.1 / 7.7.
+// 37 x 1536 x 4096 28 / 21 / 20, 1 x 1024 x 1024 7.3 / 5.1 / 7.7.  32 / 16: 1 x 1536 x 4096 10.9 / 7.5, 37 x 1536 x 4096 21.6 / 15.9, 8 x 4096 x 4096 13.1 / 9.4, 64 x 512 x 8192 44.6 / 37.4,
+// 1 x 5120 x 25600 56.5 / 65.9, 64 x 8192 x 4096 28.0 / 38.8.
 template <bool IMAGE>
 void launch(LinearProblems& ps, hipStream_t st) {
   int64_t m = 0;
   for (int i = 0; i < ps.n; ++i) m = std::max(m, ps.pr[i].m);
-  if (linear_few_wide(ps.pr[0].n)) {
+  auto with = [&](auto un, auto ahead) {
+    constexpr int UN = un(), AHEAD = ahead();
     if (m <= 16)
-      launch<IMAGE, 1, 4, 2>(ps, st);
+      launch<IMAGE, 1, UN, 2 * AHEAD>(ps, st);
     else if (m <= 32)
-      launch<IMAGE, 2, 4, 2>(ps, st);
+      launch<IMAGE, 2, UN, 2>(ps, st);
     else
-      launch<IMAGE, 4, 4, 1>(ps, st);
-  } else {
-    if (m <= 16)
-      launch<IMAGE, 1, 2, 2>(ps, st);
-    else if (m <= 32)
-      launch<IMAGE, 2, 2, 2>(ps, st);
-    else
-      launch<IMAGE, 4, 2, 1>(ps, st);
+      launch<IMAGE, 4, UN, AHEAD>(ps, st);
+  };
+  using std::integral_constant;
+  switch (linear_few_width(ps.pr[0].n, ps.pr[0].end.pre.codes != nullptr)) {
+    case 0: return with(integral_constant<int, 1>{}, integral_constant<int, 2>{});
+    case 1: return with(integral_constant<int, 2>{}, integral_constant<int, 1>{});
+    default: return with(integral_constant<int, 4>{}, integral_constant<int, 1>{});
   }
 }
 

@@ -13,7 +13,8 @@ constexpr int LINEAR_ROUND = 128;   // k of a round of a ring of two stages
 // The kernel for few rows takes up to this many rows of A, where both operands are contiguous along k.
 constexpr int LINEAR_FEW = 64;
 constexpr bool linear_few(int64_t m, bool a_trans, bool b_trans) { return m <= LINEAR_FEW && !a_trans && !b_trans; }
-constexpr bool linear_few_wide(int64_t n) { return n >= 12288; }   // blocks of 64 rows of B instead of 32 (figures at the kernel)
+// Its blocks have 16, 32 or 64 rows of B (figures at the kernel); an image's block of 32 elements is one block's.
+constexpr int linear_few_width(int64_t n, bool pre) { return n <= 4096 && !pre ? 0 : n < 12288 ? 1 : 2; }
 
 // ns that a launch takes by the tiles it has, for `steps` of 32 k.  256 x 256 in rounds of one to a CU, of which beginning and end are not hidden; 128 x 128 one to a CU with a ring of four
 // stages, or two to a CU with two.  us measured (large; small): 4096 x 4096 x 256 18; 19, x 1024 34; 39, x 4096 99; 117; 8192 x 4096 x 512 42; 48; 2048 x 4096 x 1024 35; 21, x 4096 88; 60; 1024 x 4096 x
@@ -35,6 +36,10 @@ constexpr int64_t linear_whole_rounds(int64_t large, int64_t steps) {
 constexpr bool linear_large_tiles(int64_t large, int64_t small, int64_t steps) {
   return (linear_whole_rounds(large, steps) > 0 ? linear_quarters_ns(large, steps) : linear_large_ns(large, steps)) < linear_small_ns(small, steps);
 }
+
+// Whether small tiles are done one to a CU with a ring of four stages where there are more of them than CUs: where the longest takes as many steps as a CU's share of all.  Products of 400, 128 and
+// 1000 rows by 1536 x 4096 take 54 us like this and 66 with two to a CU, four of 1000 rows 79 and 72.
+constexpr bool linear_alone(int64_t longest, int64_t all_steps) { return longest * LINEAR_CU >= all_steps; }
 
 // How many parts k is cut into, each with fp32 sums of its own in the workspace, which are added up in order: products whose small tiles leave CUs idle for long.  A product alone decides, so
 // that its sums do not depend on what shares the call.  128 k take a tile 0.6 us, a second launch and the sums 4 to 10.

@@ -432,9 +432,9 @@ void launch(const LinearProblems& ps, bool at, bool bt, dim3 grid, hipStream_t s
   else
     launch<W, STAGES, false>(ps, at, bt, grid, st);
 }
-// `each` small tiles on every XCD
-void launch_small(const LinearProblems& ps, int64_t each, bool at, bool bt, hipStream_t st) {
-  if (N_XCD * each <= LINEAR_CU)
+// `each` small tiles on every XCD, `alone`: one to a CU at a time
+void launch_small(const LinearProblems& ps, int64_t each, bool alone, bool at, bool bt, hipStream_t st) {
+  if (alone || N_XCD * each <= LINEAR_CU)
     launch<2, 4>(ps, at, bt, tile_grid(each, LINEAR_CU), st);
   else
     launch<2, 2>(ps, at, bt, tile_grid(each, 2 * LINEAR_CU), st);
@@ -447,10 +447,11 @@ hipError_t launch_linear_tiles(LinearProblems& ps, bool a_trans, bool b_trans, h
   const int64_t large = count_tiles(ps, 256), small = count_tiles(ps, 128);
   int64_t steps = 0;   // of all small tiles
   for (int i = 0; i < ps.n; ++i) steps += static_cast<int64_t>(ps.first_tile[i + 1] - ps.first_tile[i]) * ps.pr[i].steps;
+  const bool alone = linear_alone(ps.pr[0].steps, steps);
   steps = (steps + small - 1) / small;
   ps.from = 0, ps.to = longest_share(ps), ps.quarters = 0;
   if (!linear_large_tiles(large, small, steps)) {
-    launch_small(ps, ps.to, a_trans, b_trans, st);
+    launch_small(ps, ps.to, alone, a_trans, b_trans, st);
     return hipGetLastError();
   }
   count_tiles(ps, 256);
@@ -459,7 +460,7 @@ hipError_t launch_linear_tiles(LinearProblems& ps, bool a_trans, bool b_trans, h
   launch<4, 2>(ps, a_trans, b_trans, tile_grid(ps.to, LINEAR_CU), st);
   if (ps.to < all) {   // what the last round would leave most CUs without
     ps.from = ps.to, ps.to = all, ps.quarters = 1;
-    launch_small(ps, int64_t{4} * (ps.to - ps.from), a_trans, b_trans, st);
+    launch_small(ps, int64_t{4} * (ps.to - ps.from), false, a_trans, b_trans, st);
   }
   return hipGetLastError();
 }
