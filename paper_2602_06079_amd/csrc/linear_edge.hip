@@ -41,7 +41,7 @@ __global__ __launch_bounds__(EACH_THREADS) void k_linear_join(LinearJoins) {
   int j = 0;
   while (blockIdx.x >= js->first_block[j + 1]) ++j;
   const auto& q = js->jn[j];
-  const Spot s = spot(blockIdx.x - js->first_block[j], q.log_tx, q.across, 1);
+  const Spot s = spot(blockIdx.x - js->first_block[j], q.log_tx, q.across);
   const int64_t part_elements = q.m * q.pitch;
   const int parts = q.parts;
   f32x8 z[1] = {f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
@@ -155,7 +155,7 @@ hipError_t launch_linear_joins(LinearJoins& js, hipStream_t st) {
   LinearJoins rest;
   rest.n = 0;
   for (int i = 0; i < js.n; ++i) {
-    const Cover c = cover(js.jn[i].m, js.jn[i].n, 1);
+    const Cover c = cover(js.jn[i].m, js.jn[i].n);
     if (blocks + c.blocks > MOST_BLOCKS) {
       rest.n = js.n - i, js.n = i;
       std::copy_n(js.jn + i, rest.n, rest.jn);

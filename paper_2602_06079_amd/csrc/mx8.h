@@ -161,22 +161,21 @@ struct Cover {
   int across;        // blocks along a row
   int64_t blocks;
 };
-inline Cover cover(int64_t rows, int64_t cols, int rows_a_thread) {
+inline Cover cover(int64_t rows, int64_t cols) {
   const int64_t pieces = mx8_pitch(cols) / PIECE;   // a multiple of 16
   int log_tx = 8;
   while (pieces % (int64_t{1} << log_tx) != 0) --log_tx;
-  const int64_t across = pieces >> log_tx, high = (EACH_THREADS >> log_tx) * rows_a_thread;
+  const int64_t across = pieces >> log_tx, high = EACH_THREADS >> log_tx;
   return Cover{log_tx, static_cast<int>(across), across * ((rows + high - 1) / high)};
 }
-// This thread's first row and its column.
+// This thread's row (there may be none) and its column.
 struct Spot {
   int64_t row, col;
-  int step;   // rows from one of the thread's rows to the next
 };
-__device__ __forceinline__ Spot spot(unsigned block, int log_tx, int across, int rows_a_thread) {
+__device__ __forceinline__ Spot spot(unsigned block, int log_tx, int across) {
   const unsigned down = block / static_cast<unsigned>(across), along = block - down * across;
-  const int ty = threadIdx.x >> log_tx, tx = threadIdx.x & ((1 << log_tx) - 1), high = EACH_THREADS >> log_tx;
-  return Spot{static_cast<int64_t>(down) * high * rows_a_thread + ty, ((static_cast<int64_t>(along) << log_tx) + tx) * PIECE, high};
+  const int ty = threadIdx.x >> log_tx, tx = threadIdx.x & ((1 << log_tx) - 1);
+  return Spot{static_cast<int64_t>(down) * (EACH_THREADS >> log_tx) + ty, ((static_cast<int64_t>(along) << log_tx) + tx) * PIECE};
 }
 
 // Checks that the entry points share.

@@ -18,14 +18,14 @@ namespace {
 // few with much.
 template <typename E>
 __global__ __launch_bounds__(EACH_THREADS) void k_mx8_store(const E* mat, int64_t ld, Image8 image, int64_t rows, int64_t cols, int log_tx, int across) {
-  const Spot s = spot(blockIdx.x, log_tx, across, 1);
+  const Spot s = spot(blockIdx.x, log_tx, across);
   if (s.row >= rows) return;   // a row's quads are whole
   store_codes(image, s.row, s.col, cols, round8(widen(load_raw(mat + s.row * ld + s.col, cols - s.col))));
 }
 
 template <typename E>
 __global__ __launch_bounds__(EACH_THREADS) void k_mx8_load(E* mat, int64_t ld, Image8 image, int64_t rows, int64_t cols, int log_tx, int across) {
-  const Spot s = spot(blockIdx.x, log_tx, across, 1);
+  const Spot s = spot(blockIdx.x, log_tx, across);
   if (s.row < rows && s.col < cols) store_piece8(mat + s.row * ld + s.col, cols - s.col, widen(load_raw(image, s.row, s.col)));
 }
 
@@ -45,7 +45,7 @@ int check_group(const canz_mx8_group& g, int idx) {
 
 template <typename E>
 void launch(const canz_mx8_group& g, bool back, hipStream_t st) {
-  const Cover c = cover(g.rows, g.cols, 1);
+  const Cover c = cover(g.rows, g.cols);
   for (int i = 0; i < g.n_mats; ++i) {
     const Image8 image = image8(g.image[i], g.rows, g.cols);
     E* const mat = static_cast<E*>(g.mat[i]);
