@@ -16,7 +16,7 @@ constexpr bool linear_few(int64_t m, bool a_trans, bool b_trans) { return m <= L
 // Its blocks have 16, 32 or 64 rows of B (figures at the kernel); an image's block of 32 elements is one block's.
 constexpr int linear_few_width(int64_t n, bool pre) { return n <= 4096 && !pre ? 0 : n < 12288 ? 1 : 2; }
 
-// ns that a launch takes by the tiles it has, for `steps` of 32 k.  256 x 256 in rounds of one to a CU, of which beginning and end are not hidden; 128 x 128 one to a CU with a ring of four
+// About how many ns a launch takes by the tiles it has, for `steps` of 32 k.  256 x 256 in rounds of one to a CU, of which beginning and end are not hidden; 128 x 128 one to a CU with a ring of four
 // stages, or two to a CU with two.  us measured (large; small): 4096 x 4096 x 256 18; 19, x 1024 34; 39, x 4096 99; 117; 8192 x 4096 x 512 42; 48; 2048 x 4096 x 1024 35; 21, x 4096 88; 60; 1024 x 4096 x
 // 4096 83; 34, x 1024 33; 13; 1024 x 1024 x 1024 32; 11; 128 x 1024 x 256 19; 8.
 constexpr int64_t linear_large_ns(int64_t tiles, int64_t steps) { return (tiles + LINEAR_CU - 1) / LINEAR_CU * (700 * steps + 10500); }
