@@ -10,41 +10,59 @@ struct ActValue {
   float value, slope;   // act(z), act'(z)
 };
 
-// e^x for the sigmoid: v_exp_f32 is good to one step, and the product in front of it is off by at most |x| 2^-24 2, that is 1.2e-6 of a result of
-// e^-10 and less of a larger one.
-__device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896f); }
+// FINE: for fp32 results of arguments that are given.  Without it the same forms lack a correction each: for results in bf16, whose rounding is off by up to 2^-8 = 3.9e-3, and for a product's z, which is off by more
+// itself (1.9e-7 of its norm in 777 x 1531 x 1000).  In fp32 act(gate) up of 8192 x 8192 takes 390 us forward and back either way; in bf16 8192 x 12288 with GELU took 323 us without
+// and 332 with its correction (and one more term), and the product of 4096 x 25600 x 5120 967 and 984.
 
-// Phi(z) and e^(-z^2 / 2).  With x = |z| / sqrt 2 the tail Phi(-|z|) is e^(-x^2) f(x), f(x) = e^(x^2) erfc(x) / 2, which is smooth in t = 1 / (1 + 0.4 x): a polynomial of degree 9
-// in t, fitted here by weighted least squares over x in 0 .. 11, is off by 3.6e-8 of it at most (2e-7 in fp32), so that Phi keeps its relative accuracy far below 0.  Behind x = 11 the
-// exponential is 0.  The library's erfc takes all of its ranges where lanes differ: 4096 x 25600 x 5120 with GELU 1017 us with it, without an activation 846.
+// 1 / (1 + e^-z); with FINE SiLU is off by 2.8e-7 of itself at most.  x log2 e is rounded for the exponential, which counts |x| 2^-24 (without the correction SiLU is off by 9.7e-7 at -12 and 3.8e-6 at -85); what the
+// rounding (of it and of log2 e) leaves out is exact in r and goes on as a factor of the power.  The factor's bounds matter where there is no r: an infinite argument, for which the power is 0 or infinite.
+template <bool FINE>
+__device__ __forceinline__ float sigmoid(float z) {
+  constexpr float LOG2E = 1.4426950216293335f, LN2 = 0.69314718055994531f, REST = 1.3349758e-8f;   // REST: (log2 e - LOG2E) ln 2
+  const float n = z * -LOG2E, power = __builtin_amdgcn_exp2f(n);
+  if constexpr (!FINE) return __builtin_amdgcn_rcpf(1.f + power);
+  const float r = __builtin_fmaf(z, -LOG2E, -n);
+  const float w = __builtin_amdgcn_fmed3f(__builtin_fmaf(r, LN2, __builtin_fmaf(z, -REST, 1.f)), 0.999f, 1.001f);
+  return __builtin_amdgcn_rcpf(__builtin_fmaf(power, w, 1.f));
+}
+
+// Phi(z) and e^(-z^2 / 2).  The tail Phi(-|z|) is e^(-z^2 / 2) f(z), f(z) = e^(z^2 / 2) erfc(|z| / sqrt 2) / 2, which is smooth in t = 1 / (1 + A |z|): a polynomial of degree 9
+// in t, fitted here by weighted least squares over |z| in 0 .. 15.6, is off by 2.1e-8 of it at most with these coefficients (A = 11/32; 2.4e-8 with 1/4, 7e-8 with 3/8).  f changes by up to 2.3 times what t
+// changes by, so that in fp32 its value is off by 5.4e-7 at most; FINE sets t right by what 1 - t (1 + A |z|) leaves, and then it is 2.6e-7 (z Phi(z) from -1/2 to 0: 2.9e-7, 7e-8 in the mean).  The exponential's argument is rounded twice, which counts
+// up to z^2 2^-24 of Phi(-|z|): its relative accuracy falls from there on, as that of any form that squares z does.  Behind 15.6 the exponential is 0.
+// The library's erfc takes all of its ranges where lanes differ: 4096 x 25600 x 5120 with GELU 1017 us with it, without an activation 846.
 struct Normal {
   float phi, density;   // density: without 1 / sqrt(2 pi)
 };
+template <bool FINE>
 __device__ __forceinline__ Normal normal(float z) {
-  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(z), 0.28284271247461901f, 1.f));
+  constexpr float A = 0.34375f;
+  const float x = FINE ? __builtin_fminf(__builtin_fabsf(z), 16.f) : __builtin_fabsf(z);   // FINE: an infinite one would leave NaN
+  float t = __builtin_amdgcn_rcpf(__builtin_fmaf(x, A, 1.f));
+  if constexpr (FINE) t = __builtin_fmaf(t, __builtin_fmaf(-t, A * x, 1.f - t), t);
   const float e = __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f);
-  float f = 0.015846358612179756f;
-  f = __builtin_fmaf(f, t, -0.045312441885471344f);
-  f = __builtin_fmaf(f, t, -0.013677749782800674f);
-  f = __builtin_fmaf(f, t, 0.11437621712684631f);
-  f = __builtin_fmaf(f, t, -0.01534305326640606f);
-  f = __builtin_fmaf(f, t, 0.12450025230646133f);
-  f = __builtin_fmaf(f, t, 0.09197775274515152f);
-  f = __builtin_fmaf(f, t, 0.11500431597232819f);
-  f = __builtin_fmaf(f, t, 0.11261897534132004f);
-  f = __builtin_fmaf(f, t, 9.37712593440665e-06f);
+  float f = -0.028713546693325043f;
+  f = __builtin_fmaf(f, t, 0.14833438396453857f);
+  f = __builtin_fmaf(f, t, -0.2812874913215637f);
+  f = __builtin_fmaf(f, t, 0.20243380963802338f);
+  f = __builtin_fmaf(f, t, -0.04788303002715111f);
+  f = __builtin_fmaf(f, t, 0.11675199866294861f);
+  f = __builtin_fmaf(f, t, 0.11549052596092224f);
+  f = __builtin_fmaf(f, t, 0.1377772092819214f);
+  f = __builtin_fmaf(f, t, 0.13709503412246704f);
+  f = __builtin_fmaf(f, t, 1.0978608315781457e-06f);
   f *= e;
   return Normal{z > 0.f ? 1.f - f : f, e};
 }
 
-template <int ACT>
+template <int ACT, bool FINE>
 __device__ __forceinline__ ActValue act_both(float z) {
   if constexpr (ACT == CANZ_ACT_SILU) {
-    const float p = __builtin_amdgcn_rcpf(1.f + exp_fast(-z));
+    const float p = sigmoid<FINE>(z);
     const float v = z * p;
     return ActValue{v, __builtin_fmaf(v, 1.f - p, p)};
   } else if constexpr (ACT == CANZ_ACT_GELU) {
-    const Normal n = normal(z);
+    const Normal n = normal<FINE>(z);
     return ActValue{z * n.phi, __builtin_fmaf(z * 0.39894228040143268f, n.density, n.phi)};
   } else if constexpr (ACT == CANZ_ACT_RELU) {
     const bool nan = z != z;

@@ -35,7 +35,7 @@ __global__ __launch_bounds__(EACH_THREADS) void k_act_forward(Forward a) {
     f32x8 v;
 #pragma unroll
     for (int e = 0; e < PIECE; ++e) {
-      const float t = act_both<ACT>(g[e]).value;
+      const float t = act_both<ACT, std::is_same_v<E, float>>(g[e]).value;
       v[e] = UP ? t * u[e] : t;
     }
     store_piece8(static_cast<E*>(a.out) + s.row * a.ld_out + s.col, left, v);
@@ -73,7 +73,7 @@ __global__ __launch_bounds__(EACH_THREADS) void k_act_backward(Backward a) {
   if (a.dout) d = widen(dout);
 #pragma unroll
   for (int e = 0; e < PIECE; ++e) {
-    const ActValue t = act_both<ACT>(g[e]);
+    const ActValue t = act_both<ACT, std::is_same_v<E, float>>(g[e]);
     value[e] = t.value, slope[e] = t.slope;
   }
   f32x8 v;

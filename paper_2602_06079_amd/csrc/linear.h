@@ -130,7 +130,7 @@ __device__ __forceinline__ void linear_end(const LinearEnd& e, int64_t row, int 
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
-      for (int i = 0; i < PIECE; ++i) z[r][i] = act_both<decltype(kind)::value>(z[r][i]).value;
+      for (int i = 0; i < PIECE; ++i) z[r][i] = act_both<decltype(kind)::value, false>(z[r][i]).value;
   };
   if (e.act == CANZ_ACT_SILU)
     apply(std::integral_constant<int, CANZ_ACT_SILU>{});
