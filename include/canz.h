@@ -596,6 +596,8 @@ int canz_muon_step_images(const canz_group* g, int32_t n_groups, const canz_muon
  * at most 2^-4 of itself or 2^-10 X (magnitudes above 448 2^119 = 2.98e38 become that).  Every value is finite and exact in fp32 and in bf16.  A block that holds an infinity or a NaN is NaN as a
  * whole (byte 255, codes 0).  In memory: the codes row by row, rows padded to multiples of 128 bytes, then the scale bytes row by row, a
  * 32nd of that; padding is written as zeros with scale 0, and has to be that in an image that comes from elsewhere.  Images may be copied and sent as canz_mx_eight_bytes() bytes.
+ * An image that comes from elsewhere may have any scale byte and any code (127 and 255 are NaN): its values are taken in fp32, where those above its range (bytes from 247 on) are infinite,
+ * and by canz_linear in bf16, where those of bytes 0, 1 and 2 are rounded to multiples of 2^-133.
  */
 
 /* Bytes of an 8-bit image of `rows` x `cols` elements (a multiple of 256; 0 if an extent is 0). */

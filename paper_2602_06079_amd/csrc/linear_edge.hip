@@ -25,7 +25,7 @@ __global__ __launch_bounds__(EACH_THREADS) void k_linear_copy(LinearCopies) {
     const Image8 im{const_cast<uint8_t*>(static_cast<const uint8_t*>(c.from)), const_cast<uint8_t*>(c.scales), pitch};
     const f32x8 x = widen(load_raw(im, row, col));
 #pragma unroll
-    for (int e = 0; e < PIECE; ++e) v[e] = static_cast<__bf16>(col + e < c.cols ? x[e] : 0.f);   // exact; a NaN block's padding is not NaN
+    for (int e = 0; e < PIECE; ++e) v[e] = static_cast<__bf16>(col + e < c.cols ? x[e] : 0.f);   // exact but for blocks below 2^-124, which images made elsewhere may have; a NaN block's padding is not NaN
   } else {
     v = load_raw(static_cast<const __bf16*>(c.from) + row * c.ld + col, c.cols - col).v;
   }

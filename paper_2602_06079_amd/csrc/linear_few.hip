@@ -32,7 +32,7 @@ __device__ __forceinline__ bf16x8 operand(const RawA<true>& r, unsigned scale) {
   const f32x8 v = values8(r.codes, scale);
   bf16x8 o;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) o[e] = static_cast<__bf16>(v[e]);   // exact
+  for (int e = 0; e < 8; ++e) o[e] = static_cast<__bf16>(v[e]);   // exact but for blocks below 2^-124, which images made elsewhere may have
   return o;
 }
 

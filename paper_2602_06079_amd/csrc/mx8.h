@@ -131,10 +131,10 @@ __device__ __forceinline__ void store_codes(const Image8& im, int64_t row, int64
   if ((col & (MX8_BLOCK - 1)) == 0) im.scales[row * (im.pitch / MX8_BLOCK) + col / MX8_BLOCK] = col < cols ? static_cast<uint8_t>(c.scale) : 0;
 }
 
-// The values of eight codes: X times a code of 4 significant bits is exact in fp32 for every byte.
+// The values of eight codes, exact in fp32: X times a code of 4 significant bits, at least 2^-127 2^-9; from byte 247 on, which images made elsewhere may have, the largest are infinities.
 __device__ __forceinline__ f32x8 values8(u32x2 codes, unsigned scale) {
-  // byte 255 has the exponent field of an infinity; it stands for NaN
-  const float x = __builtin_bit_cast(float, scale == 255u ? 0x7FC00000u : scale << 23);
+  // byte 255 has the exponent field of an infinity; it stands for NaN.  Byte 0 has that of a subnormal number, 2^-127 with the mantissa 1/2
+  const float x = __builtin_bit_cast(float, scale == 255u ? 0x7FC00000u : max(scale << 23, 0x00400000u));
   f32x8 v;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
