@@ -110,10 +110,9 @@ int workspace_of(const canz_linear_group* g, int32_t n_groups, size_t* bytes_out
   return CANZ_OK;
 }
 
-// The launches that a product may be part of.
-enum Kind { JOIN, TILES, FEW = TILES + 4, KINDS = FEW + 6 };
+// The launches that a product with a k may be part of.
+enum Kind { TILES, FEW = TILES + 4, KINDS = FEW + 6 };
 int kind_of(const canz_linear_group& g) {
-  if (g.k == 0) return JOIN;
   if (!runs_few(g)) return TILES + 2 * g.a_trans + g.b_trans;
   return FEW + (g.a_dtype == CANZ_DT_MX8 ? 3 : 0) + linear_few_width(g.n, g.pre8 != nullptr);
 }
