@@ -194,7 +194,8 @@ struct Reader {
 
 // acc += P Q^T.  ASM: accumulators that fill one half of the registers stay there, each where it is; through the builtin the compiler moves some of them around in every round, where an
 // operand is read across k.  What it knows about these instructions and does not see here: their operands come from LDS, behind a wait; the same accumulator is needed again 63 instructions
-// later; and settle() follows every round, before anything else can read accumulators (it takes as long as the last instruction).
+// later; and settle() follows every round, before anything else can read accumulators (it takes as long as the last instruction).  tests/test_linear_hazards.py looks for these distances in
+// the assembly.
 template <bool ASM>
 __device__ __forceinline__ void multiply(f32x4& acc, const bf16x8& p, const bf16x8& q) {
   if constexpr (ASM)
