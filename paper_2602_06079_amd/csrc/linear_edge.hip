@@ -82,7 +82,7 @@ __global__ __launch_bounds__(EACH_THREADS) void k_linear_row_sums(LinearSums a) 
 }
 
 // Across k: a block has 512 columns (64 pieces) of a group of rows, of which its four wavefronts take one each by turns, eight of them on their way at a time; the groups' sums are added up by
-// k_linear_join_sums.  8192 x 12288 takes 55 us (201 MB, 3.7 TB/s) and 5 for the join.
+// k_linear_join_sums.  8192 x 12288 takes 55 us (201 MB, 3.7 TB/s) and 5 for the join behind a product; by themselves one after another 41 together.
 __global__ __launch_bounds__(EACH_THREADS) void k_linear_column_sums(LinearSums a, int across) {
   __shared__ f32x8 part[3][64];
   const unsigned group = blockIdx.x / static_cast<unsigned>(across), along = blockIdx.x - group * across;
